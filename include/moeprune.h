@@ -291,6 +291,46 @@ int skip_calibrate_beta(const float* logits, int64_t T, int E, uint32_t kept_mas
 int expert_selection_stats(const float* logits, int64_t T, int E, int k, int r, int64_t* count,
                            int64_t* coselect, uint32_t* frequency_mask, void* hip_stream);
 
+/* ---- moe_token_logprobs ------------------------------------------------------ */
+/* What a model says about given tokens: of every row z of logits [T,V], with p = softmax(z),
+ *   logprob [T] fp32 (out): log p of the row's token, tokens[t]
+ *   entropy [T] fp32 (out): -sum_i p_i log p_i (nats)
+ *   top_logprob [T,K] fp32, top_ids [T,K] int32 (out; may be NULL for K = 0): log p and index of the K
+ *     largest logits, best first, ties to the lower index
+ *   logits: row t starts ld elements after row t - 1 (ld >= V); alignment of an element suffices
+ *     (rows that start alike within 16 bytes are read fastest)
+ *   tokens [T] int64; negative: no token is given, logprob 0; V or more: NaN
+ * 0 <= K <= min(128, V); V <= 2^28.  Logits of -inf have probability 0.  A row of nothing but -inf has
+ * logprob -inf, entropy 0 and indices in ascending order; a row that holds NaN or +inf gives NaN (and
+ * indices within [0, V)).  Sums are fp32.  No workspace. */
+int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, int64_t T, int64_t V,
+                       moep_dtype dt, int K, float* logprob, float* entropy, float* top_logprob,
+                       int32_t* top_ids, void* hip_stream);
+
+/* ---- moe_distill_topk -------------------------------------------------------- */
+/* Distillation of a (pruned) student from the K best logits that a teacher gave for each token, as
+ * moe_token_logprobs keeps them.  Of every row, q = softmax(teacher / temperature) over the row's
+ * alternatives, p = softmax(logits / temperature) over all V:
+ *   loss [T] fp32 (out): temperature^2 sum_j q_j (log q_j - log p_ids[j])
+ *   stats [T,2] fp32 (out): m = max logits and log sum_i exp((logits_i - m) / temperature), for the backward call
+ *   grad [T,V] dt (out, may be NULL): weights[t] times the gradient of loss[t] by the row's logits,
+ *     weights[t] temperature (p - q); row t starts at t ld_grad; may be the logits' own memory (with ld_grad = ld)
+ *   logits: as in moe_token_logprobs;  ids [T,K] int32, teacher [T,K] fp32, 1 <= K <= 128
+ *     (logits or log probabilities: a constant added to a row of them changes nothing)
+ *   weights [T] fp32, may be NULL (1)
+ * An alternative with ids outside [0, V) or a teacher logit of -inf is not there; an id that comes several
+ * times counts as often.  A row of weight 0 is left out: its logits are not read, its loss, stats and
+ * gradient are 0.  So are loss and gradient of a row without alternatives, or of nothing but -inf.
+ * moe_distill_topk_backward: the gradient alone, from the stats of the forward call and the upstream
+ * gradient of every loss, grad_loss [T] fp32 (a row where it is 0 is not read and gets 0).  grad may be the logits' own memory. */
+int moe_distill_topk(const void* logits, int64_t ld, const int32_t* ids, const float* teacher, int64_t T,
+                     int64_t V, int K, moep_dtype dt, float temperature, const float* weights, float* loss,
+                     float* stats, void* grad, int64_t ld_grad, void* hip_stream);
+int moe_distill_topk_backward(const void* logits, int64_t ld, const int32_t* ids, const float* teacher,
+                              const float* stats, const float* grad_loss, int64_t T, int64_t V, int K,
+                              moep_dtype dt, float temperature, void* grad, int64_t ld_grad,
+                              void* hip_stream);
+
 /* ---- per-kernel timing (for benchmarks) ------------------------------------ */
 /* While enabled, every kernel launch is bracketed by HIP events on its stream.
  * moep_timing_collect waits for the recorded events, adds them up per kernel and

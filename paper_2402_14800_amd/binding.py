@@ -32,6 +32,7 @@ EXPORTS = (
     "moe_forward_skip_topk_workspace", "moe_forward_skip_topk",
     "skip_calibrate_beta_workspace", "skip_calibrate_beta", "expert_selection_stats",
     "moe_expert_outputs_ranked_workspace", "moe_expert_outputs_ranked", "prune_enumerate_ranked",
+    "moe_token_logprobs", "moe_distill_topk", "moe_distill_topk_backward",
     "moep_timing_enable", "moep_timing_collect", "moep_timing_records", "moep_mfma_ceiling",
 )
 
@@ -129,6 +130,15 @@ def _load() -> ctypes.CDLL:
     lib.prune_enumerate_ranked.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
                                            c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
                                            c_void_p, c_size_t, c_void_p]
+    lib.moe_token_logprobs.restype = c_int
+    lib.moe_token_logprobs.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int, c_int,
+                                       c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.moe_distill_topk.restype = c_int
+    lib.moe_distill_topk.argtypes = [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int64, c_int, c_int, c_float,
+                                     c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
+    lib.moe_distill_topk_backward.restype = c_int
+    lib.moe_distill_topk_backward.argtypes = [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
+                                              c_int, c_int, c_float, c_void_p, c_int64, c_void_p]
     lib.moep_timing_enable.restype = c_int
     lib.moep_timing_enable.argtypes = [c_int]
     lib.moep_timing_collect.restype = c_int
@@ -509,6 +519,85 @@ def expert_selection_stats(logits, k: int, r: Optional[int] = None):
     _check(_lib.expert_selection_stats(_ptr(logits), T, E, k, r if r is not None else 0, _ptr(count), _ptr(co),
                                        _ptr(fmask), _stream(dev)))
     return count, co, fmask
+
+
+# ---------------------------------------------------------------- logits
+def _logit_rows(logits):
+    """T, V and the distance between rows of a 2-D tensor whose rows may lie further apart than they are long."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, V]")
+    T, V = logits.shape
+    step, unit = logits.stride()
+    if not logits.is_cuda:
+        raise ValueError("all tensors must live on the same GPU")
+    if (unit != 1 and V > 1) or (step < V and T > 1):
+        raise ValueError("rows of logits must be contiguous and must not overlap")
+    return T, V, max(step, V) if T > 1 else V
+
+
+def _vector(t, shape, dtype, like, what):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+    if t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous and on the logits' GPU")
+    return t
+
+
+def moe_token_logprobs(logits, tokens, top: int = 0):
+    """logprob [T], entropy [T], top_logprob [T,top] (fp32) and top_ids [T,top] int32 of logits [T,V] at tokens [T] int64
+    (negative: none given).  Rows of logits may be views into longer rows."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    _vector(tokens, (T,), torch.int64, logits, "tokens")
+    dev = logits.device
+    logprob, entropy = torch.empty((T,), dtype=torch.float32, device=dev), torch.empty((T,), dtype=torch.float32, device=dev)
+    top_logprob = torch.empty((T, max(top, 0)), dtype=torch.float32, device=dev)
+    top_ids = torch.empty((T, max(top, 0)), dtype=torch.int32, device=dev)
+    _check(_lib.moe_token_logprobs(_ptr(logits), ld, _ptr(tokens), T, V, dt, top, _ptr(logprob), _ptr(entropy),
+                                   _ptr(top_logprob), _ptr(top_ids), _stream(dev)))
+    return logprob, entropy, top_logprob, top_ids
+
+
+def _gradient_rows(logits, grad, T: int, V: int):
+    if grad is None:
+        grad = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+    if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.get_device() != logits.get_device():
+        raise ValueError("the gradient must be like the logits")
+    return grad, _logit_rows(grad)[2]
+
+
+def moe_distill_topk(logits, ids, teacher, temperature: float = 1.0, weights=None, gradient: bool = False, out=None):
+    """loss [T] and stats [T,2] (fp32) of the student's logits [T,V] against the teacher's alternatives, ids [T,K] int32 and
+    teacher [T,K] fp32; with `gradient` also the gradient of (weights * loss).sum() by the logits, in the same pass, into
+    `out` if given (which may be `logits` itself)."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    K = ids.shape[1] if ids.dim() == 2 else 0
+    _vector(ids, (T, K), torch.int32, logits, "ids")
+    _vector(teacher, (T, K), torch.float32, logits, "teacher")
+    if weights is not None:
+        _vector(weights, (T,), torch.float32, logits, "weights")
+    dev = logits.device
+    loss, stats = torch.empty((T,), dtype=torch.float32, device=dev), torch.empty((T, 2), dtype=torch.float32, device=dev)
+    grad, ld_grad = _gradient_rows(logits, out, T, V) if gradient else (None, 0)
+    _check(_lib.moe_distill_topk(_ptr(logits), ld, _ptr(ids), _ptr(teacher), T, V, K, dt, temperature, _ptr(weights),
+                                 _ptr(loss), _ptr(stats), _ptr(grad), ld_grad, _stream(dev)))
+    return (loss, stats, grad) if gradient else (loss, stats)
+
+
+def moe_distill_topk_backward(logits, ids, teacher, stats, grad_loss, temperature: float = 1.0, out=None):
+    """The gradient [T,V] by the logits, from moe_distill_topk's stats and the upstream gradient [T] fp32 of its loss."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    K = ids.shape[1] if ids.dim() == 2 else 0
+    _vector(ids, (T, K), torch.int32, logits, "ids")
+    _vector(teacher, (T, K), torch.float32, logits, "teacher")
+    _vector(stats, (T, 2), torch.float32, logits, "stats")
+    _vector(grad_loss, (T,), torch.float32, logits, "grad_loss")
+    grad, ld_grad = _gradient_rows(logits, out, T, V)
+    _check(_lib.moe_distill_topk_backward(_ptr(logits), ld, _ptr(ids), _ptr(teacher), _ptr(stats), _ptr(grad_loss), T, V, K,
+                                          dt, temperature, _ptr(grad), ld_grad, _stream(logits.device)))
+    return grad
 
 
 # ---------------------------------------------------------------- kernel timing
