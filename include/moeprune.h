@@ -30,7 +30,7 @@
  *   - State the library keeps.  Host: the calling thread's last error message; per GPU, behind a
  *     mutex, the compute-unit count and which kernels have had their LDS limit raised (so
  *     first calls from several host threads are safe); the event pool of moep_timing_*.  Device:
- *     512 bytes of 64-bit counters in the library's own device data, through which the persistent
+ *     1024 bytes of 64-bit counters in the library's own device data, through which the persistent
  *     workgroups of the bf16 GEMM kernels line up (integer atomics on values that only grow and
  *     cannot wrap; timing depends on them, results never do), and the scratch array of
  *     prune_enumerate_static.  Calls that overlap in time on one GPU, on different streams, share
@@ -290,6 +290,28 @@ int skip_calibrate_beta(const float* logits, int64_t T, int E, uint32_t kept_mas
  * Outputs are overwritten, not accumulated.  T = 0 gives zeros. */
 int expert_selection_stats(const float* logits, int64_t T, int E, int k, int r, int64_t* count,
                            int64_t* coselect, uint32_t* frequency_mask, void* hip_stream);
+
+/* ---- expert_ffn_forward, expert_ffn_backward ----------------------------------- */
+/* One expert's gated feed-forward block on rows of its own, y = (silu(x W1^T) * (x W3^T)) W2^T, and its
+ * gradients: what fine-tuning the experts that pruning kept needs.
+ *   x [T,H], W1, W3 [F,H], W2 [H,F], y [T,H]   (dt)
+ *   gate_up [2,T,F] fp32 (out, may be NULL): x W1^T and x W3^T, for the backward call.  In bf16 they would leave
+ *     the gradients with twice the error of rounding once.
+ * Forward, bf16: the rows moe_expert_outputs gives this expert up to rounding (long sums may be cut into
+ * ranges that are added afterwards).  A row's output may depend in its last bits on how many rows the call has.
+ * Backward, from dy [T,H] (dt), the gradient of y:
+ *   dx [T,H] (dt, out, may be NULL: not wanted)
+ *   dW1, dW3 [F,H], dW2 [H,F] (dt, out, all three or none): overwritten, not accumulated; zero for T = 0
+ * Sums are fp32; da, db and h (the gradients of the branches and the product) are rounded to dt once, as the
+ * GEMMs read them, and the outputs once.  All operands 16-byte aligned; none of the outputs may overlap an input.
+ * Workspace: the matching queries (`keep`: whether gate_up is wanted). */
+size_t expert_ffn_forward_workspace(int64_t T, int H, int F, moep_dtype dt, int keep);
+int expert_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2, int64_t T, int H, int F,
+                       moep_dtype dt, void* y, float* gate_up, void* ws, size_t ws_bytes, void* hip_stream);
+size_t expert_ffn_backward_workspace(int64_t T, int H, int F, moep_dtype dt);
+int expert_ffn_backward(const void* dy, const void* x, const void* W1, const void* W3, const void* W2,
+                        const float* gate_up, int64_t T, int H, int F, moep_dtype dt, void* dx, void* dW1,
+                        void* dW3, void* dW2, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* ---- moe_token_logprobs ------------------------------------------------------ */
 /* What a model says about given tokens: of every row z of logits [T,V], with p = softmax(z),

@@ -12,6 +12,7 @@ _BINDING_NAMES = (
     "moe_pack_weights", "moe_forward_pruned_skip_packed", "moe_expert_outputs_packed",
     "moe_forward_skip_topk", "skip_calibrate_beta", "expert_selection_stats",
     "moe_expert_outputs_ranked", "prune_enumerate_ranked",
+    "expert_ffn_forward", "expert_ffn_backward",
     "moe_token_logprobs", "moe_distill_topk", "moe_distill_topk_backward",
     "num_subsets", "subset_unrank", "subset_rank", "library_path", "MoepError",
     "kernel_timing_enable", "kernel_timing_collect", "kernel_timing_reset", "kernel_timing_records", "mfma_ceiling",

@@ -33,6 +33,7 @@ EXPORTS = (
     "skip_calibrate_beta_workspace", "skip_calibrate_beta", "expert_selection_stats",
     "moe_expert_outputs_ranked_workspace", "moe_expert_outputs_ranked", "prune_enumerate_ranked",
     "moe_token_logprobs", "moe_distill_topk", "moe_distill_topk_backward",
+    "expert_ffn_forward_workspace", "expert_ffn_forward", "expert_ffn_backward_workspace", "expert_ffn_backward",
     "moep_timing_enable", "moep_timing_collect", "moep_timing_records", "moep_mfma_ceiling",
 )
 
@@ -130,6 +131,14 @@ def _load() -> ctypes.CDLL:
     lib.prune_enumerate_ranked.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
                                            c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
                                            c_void_p, c_size_t, c_void_p]
+    lib.expert_ffn_forward_workspace.restype = c_size_t
+    lib.expert_ffn_forward_workspace.argtypes = [c_int64, c_int, c_int, c_int, c_int]
+    lib.expert_ffn_forward.restype = c_int
+    lib.expert_ffn_forward.argtypes = [c_void_p] * 4 + [c_int64, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.expert_ffn_backward_workspace.restype = c_size_t
+    lib.expert_ffn_backward_workspace.argtypes = [c_int64, c_int, c_int, c_int]
+    lib.expert_ffn_backward.restype = c_int
+    lib.expert_ffn_backward.argtypes = [c_void_p] * 6 + [c_int64, c_int, c_int, c_int] + [c_void_p] * 5 + [c_size_t, c_void_p]
     lib.moe_token_logprobs.restype = c_int
     lib.moe_token_logprobs.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int, c_int,
                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
@@ -519,6 +528,52 @@ def expert_selection_stats(logits, k: int, r: Optional[int] = None):
     _check(_lib.expert_selection_stats(_ptr(logits), T, E, k, r if r is not None else 0, _ptr(count), _ptr(co),
                                        _ptr(fmask), _stream(dev)))
     return count, co, fmask
+
+
+# ---------------------------------------------------------------- one expert's block
+def _ffn_shapes(x, W1, W3, W2, what: str):
+    dt = _dtype_code(x)
+    if x.dim() != 2 or W1.dim() != 2:
+        raise ValueError(f"{what}: x must be [T, H] and W1 [F, H]")
+    T, H = x.shape
+    F = W1.shape[0]
+    if W1.shape != (F, H) or W3.shape != (F, H) or W2.shape != (H, F) or any(w.dtype != x.dtype for w in (W1, W3, W2)):
+        raise ValueError(f"{what}: W1, W3 must be [F, H] and W2 [H, F], of x's type")
+    return T, H, F, dt
+
+
+def expert_ffn_forward_workspace(T: int, H: int, F: int, dtype_code: int, save: bool = False) -> int:
+    return int(_lib.expert_ffn_forward_workspace(T, H, F, dtype_code, 1 if save else 0))
+
+
+def expert_ffn_forward(x, W1, W3, W2, save: bool = False, workspace=None):
+    """y [T,H] of one expert's block on the rows of x [T,H]; with `save` also gate_up [2,T,F] fp32 for the backward call."""
+    dev = _dev(x, W1, W3, W2)
+    T, H, F, dt = _ffn_shapes(x, W1, W3, W2, "expert_ffn_forward")
+    y = torch.empty((T, H), dtype=x.dtype, device=dev)
+    gate_up = torch.empty((2, T, F), dtype=torch.float32, device=dev) if save else None
+    ws = _workspace(_lib.expert_ffn_forward_workspace(T, H, F, dt, 1 if save else 0), dev, workspace)
+    _check(_lib.expert_ffn_forward(_ptr(x), _ptr(W1), _ptr(W3), _ptr(W2), T, H, F, dt, _ptr(y), _ptr(gate_up),
+                                   _ptr(ws), ws.numel(), _stream(dev)))
+    return (y, gate_up) if save else y
+
+
+def expert_ffn_backward_workspace(T: int, H: int, F: int, dtype_code: int) -> int:
+    return int(_lib.expert_ffn_backward_workspace(T, H, F, dtype_code))
+
+
+def expert_ffn_backward(dy, x, W1, W3, W2, gate_up, input_gradient: bool = True, weight_gradients: bool = True, workspace=None):
+    """dx [T,H], dW1, dW3 [F,H], dW2 [H,F] from dy [T,H] and the forward call's gate_up; None for what is not asked for."""
+    dev = _dev(dy, x, W1, W3, W2, gate_up)
+    T, H, F, dt = _ffn_shapes(x, W1, W3, W2, "expert_ffn_backward")
+    if dy.shape != x.shape or dy.dtype != x.dtype or gate_up.shape != (2, T, F) or gate_up.dtype != torch.float32:
+        raise ValueError("expert_ffn_backward: dy must be like x, and gate_up [2, T, F] in float32")
+    dx = torch.empty_like(x) if input_gradient else None
+    dW1, dW3, dW2 = (torch.empty_like(w) if weight_gradients else None for w in (W1, W3, W2))
+    ws = _workspace(_lib.expert_ffn_backward_workspace(T, H, F, dt), dev, workspace)
+    _check(_lib.expert_ffn_backward(_ptr(dy), _ptr(x), _ptr(W1), _ptr(W3), _ptr(W2), _ptr(gate_up), T, H, F, dt, _ptr(dx),
+                                    _ptr(dW1), _ptr(dW3), _ptr(dW2), _ptr(ws), ws.numel(), _stream(dev)))
+    return dx, dW1, dW3, dW2
 
 
 # ---------------------------------------------------------------- logits

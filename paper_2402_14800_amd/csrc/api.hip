@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -389,6 +390,232 @@ int moe_expert_outputs_packed(const void* x, const void* Wgate, const void* pack
   if (!packed_weights) return fail(MOEP_EINVAL, "moe_expert_outputs_packed: packed_weights is NULL");
   return expert_outputs(x, Wgate, nullptr, nullptr, nullptr, packed_weights, T, E, H, F, dt, logits, Y, ws,
                         ws_bytes, hip_stream, "moe_expert_outputs_packed");
+}
+
+// ------------------------------------------------------------------ expert_ffn
+// Ranges of K for a product of `M` x `N` outputs (tile_plan.h): bf16 tiles of 256 x 256 on as many compute units, ranges of at least
+// 512; fp32 tiles of 32 x 64, four to a compute unit, ranges of at least 128.
+static int ranges_of(int64_t M, int64_t N, int64_t K, moep_dtype dt, bool any) {
+  if (dt == MOEP_BF16) return (int)k_ranges(ceil_div(M, 256) * ceil_div(N, 256), 256, ceil_div(K, 64), 8, any);
+  if (!any && K % 32) return 1;
+  return (int)k_ranges(ceil_div(M, 32) * ceil_div(N, 64), 1024, ceil_div(K, 32), 4, any);
+}
+
+// C [M,N] (dt) = A B^T, in `ranges` ranges of K through `part` (ranges [M,N] fp32 matrices; only for several ranges).  bf16: both
+// operands packed, or B row-major.
+struct Product {
+  const void* A; const void* B;
+  bool b_row_major;
+  int64_t M;
+  int N, K, ranges;
+};
+static int multiply_f32_out(const Product& q, moep_dtype dt, float* out, hipStream_t s, const char* name) {
+  const int kc = q.K / q.ranges;
+  if (dt == MOEP_BF16) {
+    PackedGemmArgs g;
+    g.A = q.A; g.B = q.B; g.b_row_major = q.b_row_major; g.C = out; g.ldc = q.N;
+    g.M = q.M; g.N = q.N; g.K = q.K; g.epilogue = EPI_STORE_F32;
+    g.experts = q.ranges; g.c_expert_bytes = q.M * q.N * 4;
+    return launch_gemm_bf16_train(g, s, name);
+  }
+  GemmArgs g;
+  g.A = q.A; g.lda = q.K; g.B0 = q.B; g.ldb = q.K; g.b_expert_stride = kc;
+  g.A_rest = (const float*)q.A + kc; g.a_expert_stride = kc;
+  g.C = out; g.ldc = q.N; g.C_rest = out + q.M * q.N; g.c_expert_stride = q.M * q.N;
+  g.M = q.M; g.N = q.N; g.K = kc; g.experts = q.ranges; g.epilogue = EPI_STORE;
+  return launch_gemm_f32(g, s, name);
+}
+static int multiply(const Product& q, moep_dtype dt, void* C, float* part, hipStream_t s, const char* name) {
+  if (q.ranges > 1) {
+    if (int st = multiply_f32_out(q, dt, part, s, name)) return st;
+    return launch_sum_parts(part, q.ranges, q.M * q.N, q.M * q.N, dt, C, s);
+  }
+  if (dt == MOEP_F32) return multiply_f32_out(q, dt, (float*)C, s, name);
+  PackedGemmArgs g;
+  g.A = q.A; g.B = q.B; g.b_row_major = q.b_row_major; g.C = C; g.ldc = q.N;
+  g.M = q.M; g.N = q.N; g.K = q.K; g.epilogue = EPI_STORE;
+  return launch_gemm_bf16_packed(g, s, name);
+}
+static size_t part_bytes(int64_t M, int64_t N, int ranges) { return ranges > 1 ? align256((size_t)ranges * M * N * 4) : 0; }
+
+static int check_ffn(const char* who, int64_t T, int H, int F, moep_dtype dt) {
+  if (!valid_shape(T, 1, H, F, dt, who)) return MOEP_EINVAL;
+  return check_alignment(H, F, dt, who);
+}
+static int check_aligned(const char* who, std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if ((uintptr_t)p & 15) return fail(MOEP_EUNSUPPORTED, "%s: operands must be 16-byte aligned", who);
+  return MOEP_OK;
+}
+
+size_t expert_ffn_forward_workspace(int64_t T, int H, int F, moep_dtype dt, int keep) {
+  if (check_ffn("expert_ffn_forward_workspace", T, H, F, dt) || T == 0) return 0;
+  if (dt == MOEP_BF16 && !keep && T <= FEW_MAX_AVERAGE) return align256((size_t)T * F * 2);
+  return align256(operand_bytes(T, F, dt)) + (dt == MOEP_BF16 ? align256(operand_bytes(T, H, dt)) : 0) +
+         part_bytes(T, H, ranges_of(T, H, F, dt, false));
+}
+
+int expert_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2, int64_t T, int H, int F, moep_dtype dt,
+                       void* y, float* gate_up, void* ws, size_t ws_bytes, void* hip_stream) {
+  const char* who = "expert_ffn_forward";
+  if (int st = check_ffn(who, T, H, F, dt)) return st;
+  if (!W1 || !W3 || !W2) return fail(MOEP_EINVAL, "%s: NULL weight pointer", who);
+  if (T == 0) return MOEP_OK;
+  if (!x || !y) return fail(MOEP_EINVAL, "%s: NULL x or y", who);
+  if (int st = check_aligned(who, {x, W1, W3, W2, y, gate_up})) return st;
+  if (int st = check_ws(ws, ws_bytes, expert_ffn_forward_workspace(T, H, F, dt, gate_up != nullptr), who)) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (dt == MOEP_BF16 && !gate_up && T <= FEW_MAX_AVERAGE) {   // (bound by the read of the weights: gemm_few.hip)
+    FewGemmArgs up;
+    up.X = x; up.ldx = H; up.W0 = W1; up.W1 = W3; up.C = ws; up.ldc = F; up.N = F; up.K = H;
+    up.epilogue = EPI_SWIGLU; up.max_rows = T;
+    if (int st = launch_gemm_few(up, s, "ffn_gate_up_few")) return st;
+    FewGemmArgs down;
+    down.X = ws; down.ldx = F; down.W0 = W2; down.C = y; down.ldc = H; down.N = H; down.K = F;
+    down.epilogue = EPI_STORE; down.max_rows = T;
+    return launch_gemm_few(down, s, "ffn_down_few");
+  }
+  char* h = (char*)ws;
+  char* rest = h + align256(operand_bytes(T, F, dt));
+  if (dt == MOEP_BF16) {
+    char* xp = rest;
+    rest += align256(operand_bytes(T, H, dt));
+    if (int st = launch_pack_a_bf16(x, H, T, H, xp, s, "pack_x")) return st;
+    PackedGemmArgs up;
+    up.A = xp; up.B = W1; up.B1 = W3; up.b_row_major = true; up.C = h;
+    up.M = T; up.N = F; up.K = H; up.epilogue = gate_up ? EPI_SWIGLU_KEEP : EPI_SWIGLU;
+    up.gate_up = gate_up;
+    if (int st = gate_up ? launch_gemm_bf16_train(up, s, "ffn_gate_up_keep") : launch_gemm_bf16_packed(up, s, "ffn_gate_up")) return st;
+  } else if (gate_up) {
+    GemmArgs up;                                  // both branches as a batch of two on the same x
+    up.A = x; up.lda = H; up.B0 = W1; up.b_expert_stride = (const float*)W3 - (const float*)W1;
+    up.C = gate_up; up.ldc = F; up.C_rest = gate_up + T * F;
+    up.M = T; up.N = F; up.K = H; up.experts = 2; up.epilogue = EPI_STORE;
+    if (int st = launch_gemm_f32(up, s, "ffn_branches")) return st;
+    if (int st = launch_silu_product(gate_up, gate_up + T * F, T * F, (float*)h, s)) return st;
+  } else {
+    GemmArgs up;
+    up.A = x; up.lda = H; up.B0 = W1; up.B1 = W3; up.C = h; up.ldc = F;
+    up.M = T; up.N = F; up.K = H; up.epilogue = EPI_SWIGLU;
+    if (int st = launch_gemm_f32(up, s, "ffn_gate_up")) return st;
+  }
+  const Product down = {h, W2, true, T, H, F, ranges_of(T, H, F, dt, false)};
+  return multiply(down, dt, y, (float*)rest, s, "ffn_down");
+}
+
+// The backward call's workspace.  `t_parts` ranges along the tokens for dW2, half as many (where even) for dW1 and dW3, which have
+// twice the tiles; K of the transposed operands is T padded to whole ranges.
+struct FfnBackwardPlan {
+  int dh_parts, dx_parts, t_parts, t_parts13;
+  int64_t Tp, rows13;                             // rows13: rows of da^T | db^T as one operand
+  size_t dy, w2t, dh, dab, w13t, x_t, dy_t, dadb_t, h_t, dx_part, w13_part, w2_part, total;
+};
+static int plan_ffn_backward(int64_t T, int H, int F, moep_dtype dt, FfnBackwardPlan* p) {
+  p->dh_parts = ranges_of(T, F, H, dt, false);
+  p->dx_parts = ranges_of(T, H, 2 * (int64_t)F, dt, false);
+  p->t_parts = ranges_of(H, F, T, dt, true);
+  p->t_parts13 = p->t_parts % 2 ? p->t_parts : p->t_parts / 2;
+  const int64_t unit = (dt == MOEP_BF16 ? 64 : p->t_parts > 1 ? 32 : 4) * (int64_t)p->t_parts;
+  p->Tp = ceil_div(T, unit) * unit;
+  if (p->Tp >= (int64_t)1 << 31) return fail(MOEP_EUNSUPPORTED, "expert_ffn_backward: T=%lld is too large", (long long)T);
+  p->rows13 = dt == MOEP_BF16 ? 2 * ceil_div(F, 256) * 256 : 2 * (int64_t)F;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
+  p->dy = take(dt == MOEP_BF16 ? operand_bytes(T, H, dt) : 0);
+  p->w2t = take(operand_bytes(F, H, dt));
+  p->dh = take((size_t)p->dh_parts * T * F * 4);
+  p->dab = take(operand_bytes(T, 2 * (int64_t)F, dt));
+  p->w13t = take(operand_bytes(H, 2 * (int64_t)F, dt));
+  p->x_t = take(operand_bytes(H, p->Tp, dt));
+  p->dy_t = take(operand_bytes(H, p->Tp, dt));
+  p->dadb_t = take(operand_bytes(p->rows13, p->Tp, dt));
+  p->h_t = take(operand_bytes(F, p->Tp, dt));
+  p->dx_part = take(part_bytes(T, H, p->dx_parts));
+  p->w13_part = take(part_bytes(p->rows13, H, p->t_parts13));
+  p->w2_part = take(part_bytes(H, F, p->t_parts));
+  p->total = at;
+  return MOEP_OK;
+}
+
+size_t expert_ffn_backward_workspace(int64_t T, int H, int F, moep_dtype dt) {
+  FfnBackwardPlan p;
+  if (check_ffn("expert_ffn_backward_workspace", T, H, F, dt) || T == 0 || plan_ffn_backward(T, H, F, dt, &p)) return 0;
+  return p.total;
+}
+
+int expert_ffn_backward(const void* dy, const void* x, const void* W1, const void* W3, const void* W2, const float* gate_up,
+                        int64_t T, int H, int F, moep_dtype dt, void* dx, void* dW1, void* dW3, void* dW2, void* ws,
+                        size_t ws_bytes, void* hip_stream) {
+  const char* who = "expert_ffn_backward";
+  if (int st = check_ffn(who, T, H, F, dt)) return st;
+  const bool weights = dW1 || dW3 || dW2;
+  if (weights && (!dW1 || !dW3 || !dW2)) return fail(MOEP_EINVAL, "%s: all of dW1, dW3 and dW2 or none", who);
+  if (!W1 || !W3 || !W2) return fail(MOEP_EINVAL, "%s: NULL weight pointer", who);
+  if (int st = check_aligned(who, {dy, x, W1, W3, W2, gate_up, dx, dW1, dW3, dW2})) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const size_t es = dtype_size(dt);
+  if (T == 0) {                                   // no rows: the weights' gradients are zero
+    if (weights)
+      for (void* w : {dW1, dW3, dW2})
+        if (int st = launch_clear(w, (size_t)H * F * es, s)) return st;
+    return MOEP_OK;
+  }
+  if (!dx && !weights) return MOEP_OK;
+  if (!dy || !gate_up || (weights && !x)) return fail(MOEP_EINVAL, "%s: NULL dy, x or gate_up", who);
+  FfnBackwardPlan p;
+  if (int st = plan_ffn_backward(T, H, F, dt, &p)) return st;
+  if (int st = check_ws(ws, ws_bytes, p.total, who)) return st;
+  char* const at = (char*)ws;
+  const bool bf16 = dt == MOEP_BF16;
+  auto operand = [&](size_t off, int64_t rows, int64_t K, bool weight) { Operand o; o.p = at + off; o.rows = rows; o.K = K; o.weight = weight; return o; };
+  const Operand none;
+
+  const Operand w2t = operand(p.w2t, F, H, true), dy_a = operand(p.dy, T, H, false), dy_t = operand(p.dy_t, H, p.Tp, false);
+  if (int st = launch_transpose(W2, H, F, dt, w2t, 0, H, nullptr, s, "transpose_w")) return st;
+  if (weights) {
+    if (int st = launch_transpose(dy, T, H, dt, dy_t, 0, p.Tp, bf16 ? &dy_a : nullptr, s, "transpose_tokens")) return st;
+  } else if (bf16) {
+    if (int st = launch_pack_a_bf16(dy, H, T, H, dy_a.p, s, "pack_dy")) return st;
+  }
+  float* const dh = (float*)(at + p.dh);
+  const Product q_dh = {bf16 ? dy_a.p : dy, w2t.p, false, T, F, H, p.dh_parts};
+  if (int st = multiply_f32_out(q_dh, dt, dh, s, "ffn_dh")) return st;
+
+  const Operand dab = operand(p.dab, T, 2 * (int64_t)F, false), da_t = operand(p.dadb_t, F, p.Tp, false),
+                db_t = operand(p.dadb_t + operand_bytes(p.rows13 / 2, p.Tp, dt), F, p.Tp, false), h_t = operand(p.h_t, F, p.Tp, true);
+  if (int st = launch_gradients_of_branches(dh, p.dh_parts, gate_up, gate_up + T * F, T, F, dt, dx ? dab : none, weights ? da_t : none,
+                                            weights ? db_t : none, weights ? h_t : none, s)) return st;
+  if (dx) {
+    const Operand w13t = operand(p.w13t, H, 2 * (int64_t)F, true);
+    if (int st = launch_transpose(W1, F, H, dt, w13t, 0, F, nullptr, s, "transpose_w")) return st;
+    if (int st = launch_transpose(W3, F, H, dt, w13t, F, 2 * (int64_t)F, nullptr, s, "transpose_w")) return st;
+    const Product q = {dab.p, w13t.p, false, T, H, 2 * F, p.dx_parts};
+    if (int st = multiply(q, dt, dx, (float*)(at + p.dx_part), s, "ffn_dx")) return st;
+  }
+  if (!weights) return MOEP_OK;
+  const Operand x_t = operand(p.x_t, H, p.Tp, true);
+  if (int st = launch_transpose(x, T, H, dt, x_t, 0, p.Tp, nullptr, s, "transpose_tokens")) return st;
+  if (p.t_parts13 > 1) {                          // da^T over db^T as one operand: one launch, and a sum each
+    float* const part = (float*)(at + p.w13_part);
+    const Product q = {da_t.p, x_t.p, false, p.rows13, H, (int)p.Tp, p.t_parts13};
+    if (int st = multiply_f32_out(q, dt, part, s, "ffn_dw13")) return st;
+    if (int st = launch_sum_parts(part, q.ranges, q.M * H, (int64_t)F * H, dt, dW1, s)) return st;
+    if (int st = launch_sum_parts(part + p.rows13 / 2 * H, q.ranges, q.M * H, (int64_t)F * H, dt, dW3, s)) return st;
+  } else if (bf16) {
+    PackedGemmArgs g;
+    g.A = da_t.p; g.a_expert_bytes = db_t.p - da_t.p; g.B = x_t.p; g.b_shared = true;
+    g.C = dW1; g.c_expert_bytes = (char*)dW3 - (char*)dW1; g.ldc = H;
+    g.M = F; g.N = H; g.K = (int)p.Tp; g.experts = 2; g.epilogue = EPI_STORE;
+    if (int st = launch_gemm_bf16_packed(g, s, "ffn_dw13")) return st;
+  } else {
+    GemmArgs g;
+    g.A = da_t.p; g.A_rest = db_t.p; g.lda = p.Tp; g.B0 = x_t.p;
+    g.C = dW1; g.C_rest = dW3; g.ldc = H;
+    g.M = F; g.N = H; g.K = (int)p.Tp; g.experts = 2; g.epilogue = EPI_STORE;
+    if (int st = launch_gemm_f32(g, s, "ffn_dw13")) return st;
+  }
+  const Product q = {dy_t.p, h_t.p, false, H, F, (int)p.Tp, p.t_parts};
+  return multiply(q, dt, dW2, (float*)(at + p.w2_part), s, "ffn_dw2");
 }
 
 // ------------------------------------------------------------------ prune_enumerate

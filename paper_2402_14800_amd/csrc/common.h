@@ -80,8 +80,12 @@ __device__ __forceinline__ TopTwo top_two(const float (&v)[EMAX], int E, uint32_
 enum GemmEpilogue {
   EPI_STORE = 0,      // C[m,n] = acc                       (C in dt, N columns)
   EPI_SWIGLU = 1,     // C[m,n] = silu(A B0^T) * (A B1^T)    (C in dt, N columns)
-  EPI_ROWSCALE_F32 = 2  // C[m,n] = row_scale[m] * acc        (C in fp32)
+  EPI_ROWSCALE_F32 = 2, // C[m,n] = row_scale[m] * acc        (C in fp32)
+  // the bf16 GEMMs of an expert's training step
+  EPI_SWIGLU_KEEP = 3,  // EPI_SWIGLU, and both branches before the activation in fp32
+  EPI_STORE_F32 = 4     // C[m,n] = acc (C in fp32), one of `experts` sums over as many ranges of K
 };
+constexpr bool gemm_pairs(int epilogue) { return epilogue == EPI_SWIGLU || epilogue == EPI_SWIGLU_KEEP; }
 
 struct GemmArgs {
   const void* A = nullptr;       // [rows, K], leading dimension lda (elements)
@@ -105,6 +109,7 @@ struct GemmArgs {
   const void* A_rest = nullptr;
   void* C_rest = nullptr;
   int64_t a_expert_stride = 0, c_expert_stride = 0;
+  int64_t ldb = 0;                      // leading dimension of B (0: K)
   int busy_experts = 1;                 // grouped: experts that can have rows,
   bool rows_unknown = false;            //   and whether a threshold can leave them much fewer than M
 };
@@ -157,7 +162,13 @@ struct PackedGemmArgs {
   // tokens that were routed to a single expert go straight to the layer output.
   const int32_t* row_dest = nullptr;
   void* direct_out = nullptr;
+  bool b_shared = false;         // dense: every expert reads the same B
+  float* gate_up = nullptr;      // EPI_SWIGLU_KEEP: [2, M, N]
 };
+// The epilogues of the training step (dense): EPI_SWIGLU_KEEP on row-major weights; EPI_STORE_F32, where `experts` ranges of K
+// of ONE GEMM (K and the operands are the whole ones) give as many sums of products, c_expert_bytes apart.
+int launch_gemm_bf16_train(const PackedGemmArgs& g, hipStream_t s, const char* name);
+int allow_train_gemms();           // (by gemm_device_ready)
 size_t packed_a_bytes(int64_t rows, int K);
 size_t packed_b_bytes(int N, int K, bool gate_up_pair);
 int launch_pack_a_bf16(const void* X, int64_t ld, int64_t rows, int K, void* dst, hipStream_t s, const char* name);
@@ -293,6 +304,28 @@ int launch_calibrate_beta(const float* logits, int64_t T, int E, uint32_t kept_m
 // ---- selection statistics ---------------------------------------------------------------
 int launch_selection_stats(const float* logits, int64_t T, int E, int k, int r, int64_t* count, int64_t* co,
                            uint32_t* freq_mask, hipStream_t s);
+
+// ---- training one expert (expert_train.hip) ------------------------------------------------
+// An operand [rows, K] of a GEMM as that reads it: bf16 blocked (`weight`: with the row order of a weight's blocks), fp32
+// row-major with K elements a row.
+struct Operand {
+  char* p = nullptr;
+  int64_t rows = 0, K = 0;
+  bool weight = false;
+};
+size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt);
+// X [R, C] transposed into columns k0 .. of `out` (rows C, K at least k0 + R; columns k0 + R .. k_end - 1 are cleared); `straight`
+// (bf16, may be NULL): X itself as an operand of R rows as well.
+int launch_transpose(const void* X, int64_t R, int C, moep_dtype dt, const Operand& out, int64_t k0, int64_t k_end, const Operand* straight,
+                     hipStream_t s, const char* name);
+// From dh [parts, T, F] fp32 (to be summed) and the branches g, u [T, F] fp32: da and db as one operand [T, 2 F], and da, db and
+// h = silu(g) u transposed, [F, K] each, K >= T with zeros beyond T.
+int launch_gradients_of_branches(const float* dh, int parts, const float* g, const float* u, int64_t T, int F, moep_dtype dt, const Operand& dab,
+                                 const Operand& da_t, const Operand& db_t, const Operand& h_t, hipStream_t s);
+int launch_silu_product(const float* g, const float* u, int64_t n, float* h, hipStream_t s);
+// out[i] = sum over parts of part[p * stride + i], i < n, in that order
+int launch_sum_parts(const float* part, int parts, int64_t stride, int64_t n, moep_dtype dt, void* out, hipStream_t s);
+int launch_clear(void* p, size_t bytes, hipStream_t s);   // (bytes: a multiple of 16)
 
 // Host-side subset helpers (also used to fill the device mask table).
 int64_t binomial(int n, int r);

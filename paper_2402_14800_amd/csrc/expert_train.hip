@@ -1,0 +1,253 @@
+// What an expert's training step needs beside the GEMMs: operands transposed into the GEMMs' layouts, and the pass over the branches
+// between the two halves of the backward GEMMs.
+//
+// With g = x W1^T, u = x W3^T, h = silu(g) u, y = h W2^T and the gradient dy of y:
+//   dh = dy W2,  da = dh u s (1 + g (1 - s)) with s = 1 / (1 + exp(-g)),  db = dh g s,
+//   dx = da W1 + db W3,  dW1 = da^T x,  dW3 = db^T x,  dW2 = dy^T h.
+// The GEMMs multiply A B^T with both operands contiguous along the summed dimension, so every product but the forward's needs one or
+// both operands transposed: the weights for dh and dx, and x, dy, da, db and h along the tokens for the weights' gradients.  All of
+// these are passes bound by memory, over matrices that a GEMM reads many times.
+//
+// A thread takes a block of N x N elements (N = 8 bf16, 4 fp32: N rows of one 16-byte chunk) and transposes it in registers; lanes lie
+// so that a wavefront reads whole 128-byte lines (8 or 16 chunks side by side) and writes whole 64-byte rows of the operand's blocks.
+#include "common.h"
+
+namespace moep {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;   // one 16-byte chunk
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+template <typename S> constexpr int N_OF = 16 / sizeof(S);         // elements of a chunk
+
+// Chunk of row `row` that begins at k (a multiple of N) of an operand.  bf16: blocks of 256 rows x 32 k (gemm_packed_kernel.h), a weight's
+// rows reordered inside every 32: row 8 q + 4 b + f of them lies at 16 b + 4 q + f.
+template <typename S>
+__device__ __forceinline__ u32x4* chunk_of(const Operand& o, int64_t row, int64_t k) {
+  if constexpr (sizeof(S) == 4) return (u32x4*)(o.p + (row * o.K + k) * 4);
+  int p = (int)(row & 255);
+  if (o.weight) p = (p & ~31) | ((p & 4) << 2) | ((p & 24) >> 1) | (p & 3);
+  const int64_t block = (row >> 8) * (o.K >> 5) + (k >> 5);
+  return (u32x4*)(o.p + (block << 14) + p * 64 + ((((int)(k >> 3) & 3) ^ ((p >> 2) & 3)) << 4));
+}
+
+// in[i] = row i of the block, out[j] = its column j
+template <typename S>
+__device__ __forceinline__ void transposed(const u32x4 (&in)[N_OF<S>], u32x4 (&out)[N_OF<S>]) {
+  if constexpr (sizeof(S) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = u32x4{in[0][j], in[1][j], in[2][j], in[3][j]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)                            // (bytes of the first row's element below those of the second's)
+        out[j][q] = __builtin_amdgcn_perm(in[2 * q + 1][j >> 1], in[2 * q][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+  }
+}
+
+// Where a thread's block lies: workgroups walk 256 columns x N^2 rows, a wavefront 64 columns, 64 / N chunks side by side.
+template <typename S>
+struct Place {
+  int64_t r0;
+  int c0;
+  __device__ Place() {
+    constexpr int N = N_OF<S>, SIDE = 64 / N;
+    const int lane = threadIdx.x & 63;
+    r0 = (int64_t)blockIdx.x * (N * N) + (lane / SIDE) * N;
+    c0 = blockIdx.y * 256 + (threadIdx.x >> 6) * 64 + (lane % SIDE) * N;
+  }
+};
+template <typename S>
+dim3 grid_of(int64_t rows, int64_t columns) {
+  return dim3((unsigned)ceil_div(rows, (int64_t)N_OF<S> * N_OF<S>), (unsigned)ceil_div(columns, 256));
+}
+
+struct TransposeArgs {
+  const char* X;
+  int64_t R, k0, k_end;
+  int C;
+  Operand out, straight;
+};
+
+template <typename S>
+__global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs p) {
+  constexpr int N = N_OF<S>;
+  const Place<S> at;
+  if (at.c0 >= p.C) return;
+  u32x4 in[N], out[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    in[i] = u32x4{0, 0, 0, 0};
+    const int64_t r = at.r0 + i;
+    if (r < p.R) {
+      in[i] = *(const u32x4*)(p.X + (r * p.C + at.c0) * sizeof(S));
+      if (p.straight.p) *chunk_of<S>(p.straight, r, at.c0) = in[i];
+    }
+  }
+  if (p.k0 + at.r0 >= p.k_end) return;
+  transposed<S>(in, out);
+#pragma unroll
+  for (int j = 0; j < N; ++j) *chunk_of<S>(p.out, at.c0 + j, p.k0 + at.r0) = out[j];
+}
+
+struct BranchArgs {
+  const float* dh; const float* g; const float* u;
+  int parts, F;
+  int64_t T, part_stride;
+  Operand dab, da_t, db_t, h_t;
+};
+
+template <typename S>
+__device__ __forceinline__ u32x4 rounded(const float (&x)[N_OF<S>]) {
+  u32x4 v;
+  if constexpr (sizeof(S) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, bf16x2));
+  }
+  return v;
+}
+
+// Reads 12 bytes an element (dh, g, u in fp32: rounded to bf16 before this pass they would leave the gradients with twice the error of
+// one rounding) and writes five chunks' worth: da, db as the A operand of dx, da, db, h along the tokens.
+template <typename S>
+__global__ __launch_bounds__(256) void branch_gradients_kernel(BranchArgs p) {
+  constexpr int N = N_OF<S>;
+  const Place<S> at;
+  if (at.c0 >= p.F || at.r0 >= p.da_t.K) return;
+  u32x4 a[N], b[N], h[N], out[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    a[i] = b[i] = h[i] = u32x4{0, 0, 0, 0};
+    const int64_t t = at.r0 + i;
+    if (t < p.T) {
+      const int64_t e = t * p.F + at.c0;
+      float dh[N], g[N], u[N], xa[N], xb[N], xh[N];
+#pragma unroll
+      for (int j = 0; j < N; j += 4) {
+        *(f32x4*)(dh + j) = *(const f32x4*)(p.dh + e + j);
+        *(f32x4*)(g + j) = *(const f32x4*)(p.g + e + j);
+        *(f32x4*)(u + j) = *(const f32x4*)(p.u + e + j);
+      }
+      for (int q = 1; q < p.parts; ++q)
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+          const f32x4 x = *(const f32x4*)(p.dh + q * p.part_stride + e + j);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) dh[j + v] += x[v];
+        }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float s = 1.f / (1.f + __expf(-g[j])), silu = g[j] * s;
+        xa[j] = dh[j] * u[j] * (s * (1.f + g[j] * (1.f - s)));
+        xb[j] = dh[j] * silu;
+        xh[j] = silu * u[j];
+      }
+      a[i] = rounded<S>(xa); b[i] = rounded<S>(xb); h[i] = rounded<S>(xh);
+      if (p.dab.p) {
+        *chunk_of<S>(p.dab, t, at.c0) = a[i];
+        *chunk_of<S>(p.dab, t, p.F + at.c0) = b[i];
+      }
+    }
+  }
+  if (!p.da_t.p) return;
+  auto put = [&](const u32x4 (&in)[N], const Operand& o) {
+    transposed<S>(in, out);
+#pragma unroll
+    for (int j = 0; j < N; ++j) *chunk_of<S>(o, at.c0 + j, at.r0) = out[j];
+  };
+  put(a, p.da_t);
+  put(b, p.db_t);
+  put(h, p.h_t);
+}
+
+__global__ __launch_bounds__(256) void silu_product_kernel(const f32x4* g, const f32x4* u, int64_t n, f32x4* h) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const f32x4 a = g[i], b = u[i];
+  f32x4 o;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) o[v] = a[v] / (1.f + expf(-a[v])) * b[v];
+  h[i] = o;
+}
+
+template <typename S>
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* part, int parts, int64_t stride, int64_t n, S* out) {
+  constexpr int N = N_OF<S>;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
+  if (i >= n) return;
+  float x[N];
+#pragma unroll
+  for (int j = 0; j < N; j += 4) *(f32x4*)(x + j) = *(const f32x4*)(part + i + j);
+  for (int q = 1; q < parts; ++q)
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+      const f32x4 y = *(const f32x4*)(part + q * stride + i + j);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) x[j + v] += y[v];
+    }
+  *(u32x4*)(out + i) = rounded<S>(x);
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(u32x4* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = u32x4{0, 0, 0, 0};
+}
+
+}  // namespace
+
+size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt) {
+  return dt == MOEP_BF16 ? (size_t)ceil_div(rows, 256) * 256 * (size_t)K * 2 : (size_t)rows * (size_t)K * 4;
+}
+
+int launch_transpose(const void* X, int64_t R, int C, moep_dtype dt, const Operand& out, int64_t k0, int64_t k_end, const Operand* straight,
+                     hipStream_t s, const char* name) {
+  TransposeArgs p = {(const char*)X, R, k0, k_end, C, out, straight ? *straight : Operand{}};
+  Timed t(name, s);
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(transpose_kernel<uint16_t>, grid_of<uint16_t>(k_end - k0, C), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(transpose_kernel<float>, grid_of<float>(k_end - k0, C), dim3(256), 0, s, p);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+int launch_gradients_of_branches(const float* dh, int parts, const float* g, const float* u, int64_t T, int F, moep_dtype dt, const Operand& dab,
+                                 const Operand& da_t, const Operand& db_t, const Operand& h_t, hipStream_t s) {
+  BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, dab, da_t, db_t, h_t};
+  if (!p.da_t.p) p.da_t.K = T;
+  Timed t("branch_gradients", s);
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(branch_gradients_kernel<uint16_t>, grid_of<uint16_t>(p.da_t.K, F), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(branch_gradients_kernel<float>, grid_of<float>(p.da_t.K, F), dim3(256), 0, s, p);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+int launch_silu_product(const float* g, const float* u, int64_t n, float* h, hipStream_t s) {
+  Timed t("silu_product", s);
+  hipLaunchKernelGGL(silu_product_kernel, dim3((unsigned)ceil_div(n / 4, 256)), dim3(256), 0, s, (const f32x4*)g, (const f32x4*)u, n / 4, (f32x4*)h);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+int launch_sum_parts(const float* part, int parts, int64_t stride, int64_t n, moep_dtype dt, void* out, hipStream_t s) {
+  Timed t("sum_parts", s);
+  const unsigned blocks = (unsigned)ceil_div(n, 256 * (dt == MOEP_BF16 ? 8 : 4));
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, dim3(blocks), dim3(256), 0, s, part, parts, stride, n, (uint16_t*)out);
+  else hipLaunchKernelGGL(sum_parts_kernel<float>, dim3(blocks), dim3(256), 0, s, part, parts, stride, n, (float*)out);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+int launch_clear(void* p, size_t bytes, hipStream_t s) {
+  const int64_t n = (int64_t)(bytes / 16);
+  if (!n) return MOEP_OK;
+  const int64_t blocks = ceil_div(n, 256);
+  hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, (u32x4*)p, n);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+}  // namespace moep

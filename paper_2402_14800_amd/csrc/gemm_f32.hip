@@ -30,7 +30,7 @@ struct FArgs {
   float* C;
   const float* row_scale;
   const int32_t* seg_end; int segments;                    // routed: the experts' segment ends; segments 0: dense
-  int64_t M, lda, ldc, b_expert_stride;
+  int64_t M, lda, ldb, ldc, b_expert_stride;
   const float* A_rest; float* C_rest;                      // dense, blockIdx.z = expert: experts 1, 2, ...
   int64_t a_expert_stride, c_expert_stride;
   int N, K;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(THREADS) void gemm_f32_kernel(FArgs p) {
     const float* base = EPI == EPI_SWIGLU && br >= TN ? B1 : B0;
     int n = n0 + (EPI == EPI_SWIGLU ? br % TN : br);
     if (n >= p.N) n = p.N - 1;
-    src[RT + i] = base + (int64_t)n * p.K + sc * 4;
+    src[RT + i] = base + (int64_t)n * p.ldb + sc * 4;
   }
   typedef __attribute__((address_space(3))) char lds_char;
   lds_char* const lds3 = (lds_char*)&lds[0][0] + __builtin_amdgcn_readfirstlane(wave) * 1024;
@@ -220,12 +220,13 @@ constexpr int64_t NARROW_TILES_BELOW = 512;
 int launch_gemm_f32(const GemmArgs& g, hipStream_t s, const char* name) {
   if (g.K % 4 || g.K <= 0 || g.lda % 4) return fail(MOEP_EUNSUPPORTED, "%s: K=%d and lda must be multiples of 4", name, g.K);
   if (g.N % 4 || g.ldc % 4) return fail(MOEP_EUNSUPPORTED, "%s: N=%d and ldc must be multiples of 4", name, g.N);
+  if (g.ldb % 4 || (g.ldb && g.ldb < g.K)) return fail(MOEP_EINVAL, "%s: bad leading dimension of B", name);
   if (g.M <= 0 || g.N <= 0) return MOEP_OK;
   FArgs f = {};
   f.A = (const float*)g.A; f.B0 = (const float*)g.B0; f.B1 = (const float*)g.B1;
   f.a_rows = g.a_rows; f.C = (float*)g.C; f.row_scale = g.row_scale;
   f.seg_end = g.seg_end; f.segments = g.segments;
-  f.M = g.M; f.lda = g.lda; f.ldc = g.ldc; f.b_expert_stride = g.b_expert_stride;
+  f.M = g.M; f.lda = g.lda; f.ldb = g.ldb ? g.ldb : g.K; f.ldc = g.ldc; f.b_expert_stride = g.b_expert_stride;
   f.A_rest = (const float*)g.A_rest; f.C_rest = (float*)g.C_rest;
   f.a_expert_stride = g.a_expert_stride; f.c_expert_stride = g.c_expert_stride;
   f.N = g.N; f.K = g.K;

@@ -75,4 +75,16 @@ constexpr bool f32_columns_first(bool routed, int64_t row_tiles) { return routed
 // Row tiles of a routed launch, expected: every expert's last one is half full.
 constexpr int64_t routed_row_tiles(int64_t rows, int experts, int tile_rows) { return (rows + (int64_t)experts * (tile_rows / 2)) / tile_rows; }
 
+// Ranges of K that one GEMM of `tiles` tiles is cut into, each summed by workgroups of its own and the sums added afterwards, so that
+// fewer tiles than compute units still occupy them.  `units`: steps of K that a range consists of whole numbers of, at least `least`
+// of them; `any`: K is padded to fit, else the ranges have to divide it.
+constexpr int64_t k_ranges(int64_t tiles, int64_t room, int64_t units, int64_t least, bool any) {
+  if (tiles <= 0 || 2 * tiles > room) return 1;
+  int64_t n = room / tiles;
+  if (n > units / least) n = units / least;
+  if (n < 1) n = 1;
+  while (!any && units % n) --n;
+  return n;
+}
+
 }  // namespace moep

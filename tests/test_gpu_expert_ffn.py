@@ -1,0 +1,203 @@
+"""GPU parity of one expert's block, forward and backward, with its definition in 64 bits.
+
+Bounds, per tensor.  bf16: an output is rounded once, by 2^-9 of itself at most; da, db and h were rounded once before, so a sum of
+products is off by 2^-9 of the sum of its terms' magnitudes at most, and by 2^-9 of itself in the 2-norm, the roundings being
+independent of each other: WORST bounds every element by the former, NORM the whole by sqrt(2) 2^-9 = 2.8e-3, with room for the
+exponential and fp32 sums.  What is rounded is itself computed from fp32 sums over K = H, off by K 2^-24 of their terms' magnitudes at
+the very most, which matters where da is small because silu' or dh nearly vanishes: SUMS carries that through.  fp32: sums of up to 6000 terms, each step 2^-24: 6000 2^-24 = 3.6e-4 of the magnitudes at the very most,
+sqrt(6000) 2^-24 = 5e-6 of the norm."""
+import pytest
+import torch
+
+import paper_2402_14800_amd as pkg
+from paper_2402_14800_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NORM = {torch.bfloat16: 4e-3, torch.float32: 1e-5}
+WORST = {torch.bfloat16: 2.0 ** -8, torch.float32: 3.6e-4}
+NAMES = ("y", "dx", "dW1", "dW3", "dW2")
+
+
+def make_block(T, H, F, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+    return [t.to(dtype).to(DEV) for t in (r(T, H), r(F, H) / H ** 0.5, r(F, H) / H ** 0.5, r(H, F) / F ** 0.5, r(T, H))]
+
+
+def reference(x, W1, W3, W2, dy):
+    """Outputs, the sums of their terms' magnitudes, and what the branches' sums may add to an error, in 64 bits."""
+    x, W1, W3, W2, dy = (t.double() for t in (x, W1, W3, W2, dy))
+    g, u = x @ W1.T, x @ W3.T
+    s = 1 / (1 + torch.exp(-g))
+    h, dh = g * s * u, dy @ W2
+    da, db = dh * u * (s + g * s * (1 - s)), dh * g * s
+    a = torch.abs
+    # errors of the branches' sums, carried into da, db and h (|silu'| <= 1.1, |silu''| <= 0.5)
+    sums = x.shape[1] * 2.0 ** -24
+    eg, eu, edh = sums * a(x) @ a(W1).T, sums * a(x) @ a(W3).T, sums * a(dy) @ a(W2)
+    ea = 1.1 * (edh * a(u) + a(dh) * eu) + 0.5 * a(dh * u) * eg
+    eb = edh * a(g * s) + 1.1 * a(dh) * eg
+    eh = 1.1 * eg * a(u) + a(g * s) * eu
+    ref = (h @ W2.T, da @ W1 + db @ W3, da.T @ x, db.T @ x, dy.T @ h)
+    mag = (a(h) @ a(W2).T, a(da) @ a(W1) + a(db) @ a(W3), a(da).T @ a(x), a(db).T @ a(x), a(dy).T @ a(h))
+    more = (eh @ a(W2).T, ea @ a(W1) + eb @ a(W3), ea.T @ a(x), eb.T @ a(x), a(dy).T @ eh)
+    return ref, tuple(zip(mag, more))
+
+
+def check(got, ref, mag, dtype, names=NAMES):
+    for n, o, r, (m, more) in zip(names, got, ref, mag):
+        assert o.dtype == dtype and o.shape == r.shape
+        d = (o.double() - r).abs()
+        bound = 2.0 ** -8 * r.abs() * (dtype == torch.bfloat16) + WORST[dtype] * m + more
+        assert bool((d <= bound + 1e-30).all()), (n, float((d - bound).max()))
+        assert float(d.norm()) <= NORM[dtype] * float(r.norm()) + 1e-30, (n, float(d.norm() / r.norm()))
+
+
+def workspace(nbytes):
+    """A workspace whose bytes are NaN in either type, with a tail that the call must leave alone."""
+    return torch.full((nbytes + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+
+
+def step(x, W1, W3, W2, dy):
+    T, H = x.shape
+    F = W1.shape[0]
+    code = binding._dtype_code(x)
+    n1, n2 = binding.expert_ffn_forward_workspace(T, H, F, code, True), binding.expert_ffn_backward_workspace(T, H, F, code)
+    w1, w2 = workspace(n1), workspace(n2)
+    y, gate_up = pkg.expert_ffn_forward(x, W1, W3, W2, save=True, workspace=w1[:n1])
+    grads = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up, workspace=w2[:n2])
+    torch.cuda.synchronize()
+    assert bool((w1[n1:] == 0xFF).all()) and bool((w2[n2:] == 0xFF).all())
+    return (y, *grads), gate_up
+
+
+BF16_SHAPES = [(1, 64, 64), (2, 64, 128), (3, 192, 64), (47, 128, 192), (48, 320, 832), (49, 64, 256), (63, 256, 64), (64, 128, 128),
+               (65, 576, 320), (128, 1024, 3584), (129, 64, 14336), (255, 4096, 64), (256, 512, 1024), (257, 256, 1088), (777, 1024, 3584),
+               (1, 4096, 14336), (5000, 512, 1024), (6000, 64, 128), (4097, 832, 192), (2049, 2048, 5632)]
+
+
+@pytest.mark.parametrize("T,H,F", BF16_SHAPES)
+def test_bf16_step_over_shapes(T, H, F):
+    ops = make_block(T, H, F, torch.bfloat16, seed=T)
+    got, gate_up = step(*ops)
+    ref, mag = reference(*ops)
+    check(got, ref, mag, torch.bfloat16)
+    x, W1, W3 = (t.double() for t in ops[:3])
+    for i, w in enumerate((W1, W3)):                         # fp32 sums of exact products
+        assert float((gate_up[i].double() - x @ w.T).norm()) <= 1e-5 * float((x @ w.T).norm())
+    n = binding.expert_ffn_forward_workspace(T, H, F, binding.MOEP_BF16)
+    w = workspace(n)
+    y = pkg.expert_ffn_forward(*ops[:4], workspace=w[:n])
+    torch.cuda.synchronize()
+    assert bool((w[n:] == 0xFF).all())
+    check((y,), ref, mag, torch.bfloat16)
+
+
+F32_SHAPES = [(1, 4, 4), (2, 8, 36), (3, 64, 128), (33, 100, 60), (64, 36, 260), (65, 512, 64), (130, 4, 516), (513, 64, 128), (777, 128, 384),
+              (1501, 512, 1024), (4099, 64, 128), (6000, 32, 32), (100, 1024, 3584)]
+
+
+@pytest.mark.parametrize("T,H,F", F32_SHAPES)
+def test_f32_step_over_shapes(T, H, F):
+    ops = make_block(T, H, F, torch.float32, seed=T)
+    got, _ = step(*ops)
+    ref, mag = reference(*ops)
+    check(got, ref, mag, torch.float32)
+    check((pkg.expert_ffn_forward(*ops[:4]),), ref, mag, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_forward_is_the_expert_pass(dtype):
+    """The same rows from moe_expert_outputs, where neither cuts its sums into ranges: the same bits."""
+    T, H, F = 40, 256, 512
+    x, W1, W3, W2, _ = make_block(T, H, F, dtype, seed=5)
+    Y = pkg.moe_expert_outputs(x, torch.zeros((1, H), dtype=dtype, device=DEV), W1[None], W3[None], W2[None])[1]
+    y = pkg.expert_ffn_forward(x, W1, W3, W2)
+    if dtype == torch.bfloat16:
+        assert torch.equal(y, Y[0])
+    else:
+        assert float((y - Y[0]).norm()) <= NORM[dtype] * float(Y.norm())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,H,F", [(1, 64, 64), (300, 256, 512), (3000, 128, 192)])
+def test_parts_of_the_gradient(T, H, F, dtype):
+    x, W1, W3, W2, dy = make_block(T, H, F, dtype, seed=9)
+    _, gate_up = pkg.expert_ffn_forward(x, W1, W3, W2, save=True)
+    whole = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up)
+    again = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up)
+    only_x = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up, weight_gradients=False)
+    only_w = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up, input_gradient=False)
+    assert all(torch.equal(a, b) for a, b in zip(whole, again))
+    assert torch.equal(only_x[0], whole[0]) and only_x[1:] == (None, None, None)
+    assert only_w[0] is None and all(torch.equal(a, b) for a, b in zip(only_w[1:], whole[1:]))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_no_rows(dtype):
+    x, W1, W3, W2, dy = make_block(0, 64, 128, dtype)
+    y, gate_up = pkg.expert_ffn_forward(x, W1, W3, W2, save=True)
+    dx, *dW = pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up)
+    assert y.shape == dx.shape == (0, 64) and not any(bool(w.any()) for w in dW)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_steep_branches(dtype):
+    """Gates far on either side of 0: the exponential overflows or vanishes, the gradients stay finite and right."""
+    T, H, F = 70, 64, 128
+    x, W1, W3, W2, dy = make_block(T, H, F, dtype, seed=13)
+    W1 *= 100
+    got, _ = step(x, W1, W3, W2, dy)
+    assert all(bool(torch.isfinite(o).all()) for o in got)
+    ref, mag = reference(x, W1, W3, W2, dy)
+    check(got, ref, mag, dtype)
+
+
+def test_gradients_against_differences():
+    """L = <y, dy> along a direction d of each operand: (L(+e) - L(-e)) / 2 e = <grad, d> + O(e^2).  The block is smooth with derivatives
+    of order 1 here; with e = 2^-7 the remainder is below 2^-14 of |L'''| ~ |grad| |d|, fp32 losses off by 1e-5 |y| |dy| over 2 e."""
+    T, H, F, e = 37, 60, 92, 2.0 ** -7
+    ops = make_block(T, H, F, torch.float32, seed=17)
+    dy = ops[4]
+    (y, *grads), _ = step(*ops)
+    g = torch.Generator().manual_seed(18)
+    for i, grad in enumerate(grads):                         # x, W1, W3, W2
+        d = torch.randn(ops[i].shape, generator=g).to(DEV)
+        d /= d.norm()
+        loss = []
+        for s in (1, -1):
+            moved = list(ops[:4])
+            moved[i] = ops[i] + s * e * d
+            loss.append(float((pkg.expert_ffn_forward(*moved).double() * dy.double()).sum()))
+        want, got = (loss[0] - loss[1]) / (2 * e), float((grad.double() * d.double()).sum())
+        tol = 2.0 ** -12 * float(grad.norm()) + 1e-6 * float(y.norm()) * float(dy.norm()) / (2 * e)
+        assert abs(want - got) <= tol, (i, want, got, tol)
+
+
+def test_step_on_another_stream_and_in_a_graph():
+    ops = make_block(300, 256, 512, torch.bfloat16, seed=21)
+    run = lambda: step_plain(*ops)  # noqa: E731
+
+    def step_plain(x, W1, W3, W2, dy):
+        y, gate_up = pkg.expert_ffn_forward(x, W1, W3, W2, save=True)
+        return (y, *pkg.expert_ffn_backward(dy, x, W1, W3, W2, gate_up))
+
+    want = run()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = run()
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for seed in range(3):
+        for t, n in zip(ops, make_block(300, 256, 512, torch.bfloat16, seed=30 + seed)):
+            t.copy_(n)
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
