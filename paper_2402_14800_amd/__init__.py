@@ -24,5 +24,7 @@ def __getattr__(name):
         import importlib
 
         mod = importlib.import_module(".binding", __name__)
-        return mod if name == "binding" else getattr(mod, name)
+        value = mod if name == "binding" else getattr(mod, name)
+        globals()[name] = value              # (found directly from now on: coming here costs 4 us)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -6,11 +6,14 @@
 // tau^2 sum_j q_j (log q_j - log p_id(j)) and its gradient tau (p - q).
 //
 // Bound by the one read of the logits (and the one write of the gradient); the lanes are close behind: an element of two
-// bytes costs about ten lane operations, four of them the exponential.  One workgroup takes a row; each thread keeps its own
+// bytes costs about ten lane operations, four of them the exponential.  A workgroup takes a row; each thread keeps its own
 // running maximum and sums (a rescale per 16 chunks), so the row is read without a barrier and joined once at its end.  Up to
 // 16 chunks of 16 bytes per thread stay in registers, so a row of up to 32768 bf16 logits on 256 threads is read from memory
-// once also where it is used again (the gradient, the search for the best); a longer one is walked tile by tile and read
-// again from the caches.
+// once also where it is used again (the gradient, the search for the best); a longer one is walked tile by tile.
+// (Workgroups that stay and ask for their next row while they end the present one were slower everywhere, 1.1 to 1.7 times: loads and
+// stores return in order, so a row's first chunk waited for the stores before it. More workgroups than fit do the same without.)
+#include <type_traits>
+
 #include "common.h"
 
 namespace moep {
@@ -19,6 +22,8 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;   // one 16-byte chunk
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -33,7 +38,7 @@ template <> struct Elements<float> {
   __device__ static float get(const u32x4& v, int j) { return __uint_as_float(v[j]); }
   __device__ static float load(const float* p) { return *p; }
   __device__ static void store(float* p, float x) { *p = x; }
-  __device__ static void put(u32x4& v, int j, const float* p) { v[j] = __float_as_uint(*p); }
+  __device__ static float nothing() { return NEG_INF; }
   __device__ static u32x4 pack(const float (&x)[4]) {
     return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
   }
@@ -44,9 +49,7 @@ template <> struct Elements<uint16_t> {
   __device__ static float get(const u32x4& v, int j) { return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16); }
   __device__ static float load(const uint16_t* p) { return __uint_as_float((unsigned)*p << 16); }
   __device__ static void store(uint16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }   // (to the nearest, ties to even)
-  __device__ static void put(u32x4& v, int j, const uint16_t* p) {
-    v[j >> 1] = j & 1 ? (v[j >> 1] & 0xffffu) | ((unsigned)*p << 16) : (v[j >> 1] & 0xffff0000u) | *p;
-  }
+  __device__ static uint16_t nothing() { return 0xff80; }
   __device__ static u32x4 pack(const float (&x)[8]) {
     u32x4 v;
 #pragma unroll
@@ -57,54 +60,108 @@ template <> struct Elements<uint16_t> {
 
 // The larger one, NaN if either is (fmaxf drops a NaN): a row that holds one is told by its maximum.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// Largest halves of a chunk as signed 16-bit numbers, those of even and of odd elements.
+__device__ __forceinline__ s16x2 top_halves(const u32x4& v) {
+  const unsigned a = v[0], b = v[1], c = v[2], d = v[3];     // (numbers of their own: __builtin_bit_cast of v[i] reads v[0])
+  return __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)),
+                                   __builtin_elementwise_max(__builtin_bit_cast(s16x2, c), __builtin_bit_cast(s16x2, d)));
+}
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A row seen as 16-byte chunks from the boundary at or before its first element: chunk c holds elements c N - lead .. + N - 1,
-// of which those within [0, V) exist.  Rows need no alignment beyond their elements'.
+// of which those within [0, V) are the row's.  Rows need no alignment beyond their elements'.  A chunk that reaches beyond the row on
+// either side is loaded whole where that stays between the first row's first element and the last row's last, and cut to the row in
+// registers; only the first row's first chunk and the last row's last one are put together element by element.
 template <typename S>
 struct Row {
   static constexpr int N = Elements<S>::N;
   const S* at;
-  int V, lead, chunks, first_whole, end_whole;
-  __device__ Row(const S* p, int V_) : at(p), V(V_) {
-    lead = (int)(((uintptr_t)p & 15) / sizeof(S));
+  const char* base;                          // of chunk 0
+  int V, lead, chunks, first_load, end_load;
+  __device__ Row(const void* rows, int64_t ld, int V_, int64_t t, int64_t T) : at((const S*)rows + t * ld), V(V_) {
+    base = (const char*)at - ((uintptr_t)at & 15);
+    lead = (int)(((uintptr_t)at & 15) / sizeof(S));
     chunks = (V + lead + N - 1) / N;
-    first_whole = lead ? 1 : 0;
-    end_whole = (V + lead) / N;
+    first_load = t * ld < lead ? 1 : 0;
+    end_load = V == 0 ? 0 : (T - 1 - t) * ld + V >= (int64_t)chunks * N - lead ? chunks : (V + lead) / N;
   }
-  __device__ bool whole(int c) const { return c >= first_whole && c < end_whole; }
-  __device__ u32x4 partial(int c) const {
-    u32x4 v = {Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL};
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = c * N - lead + j;
-      if (i >= 0 && i < V) Elements<S>::put(v, j, at + i);
-    }
-    return v;
-  }
+  __device__ bool whole(int c) const { return c * N >= lead && (c + 1) * N <= V + lead; }
+  __device__ const u32x4* chunk(int c) const { return (const u32x4*)(base + (uint32_t)c * 16u); }
+  __device__ bool has(int c, int j) const { const int i = c * N - lead + j; return i >= 0 && i < V; }
 };
 
-// Chunks tile B NC + n B + tid of a row in a thread's registers; what the row does not have is -inf.
+template <typename S>
+__device__ __forceinline__ u32x4 neutral() {
+  return u32x4{Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL};
+}
+
+// Chunk c (thread by thread) of a row: the request alone, nothing waits.  What is not there is -inf.
+template <typename S>
+__device__ __forceinline__ void request(const Row<S>& row, int c, u32x4& v) {
+  v = neutral<S>();
+  if (c >= row.first_load && c < row.end_load) v = *row.chunk(c);
+}
+// Chunks tile B NC + n B + tid of a row
 template <typename S, int B>
-__device__ __forceinline__ void load_tile(const Row<S>& row, int tile, u32x4 (&v)[NC]) {
-  const int tid = threadIdx.x, c0 = tile * (B * NC) + tid;
+__device__ __forceinline__ void request_tile(const Row<S>& row, int tile, int tid, u32x4 (&v)[NC]) {
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    v[n] = u32x4{Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL};
-    const int c = c0 + n * B;
-    if (row.whole(c)) v[n] = *(const u32x4*)(row.at + ((int64_t)c * Row<S>::N - row.lead));
-  }
-  if (row.lead || row.end_whole < row.chunks) {              // the ends of the row
-    if (row.lead && c0 == 0) v[0] = row.partial(0);
-    const int last = row.end_whole;
-    if (last < row.chunks && last >= row.first_whole && last >= c0 && last < c0 + B * NC && (last - c0) % B == 0) {
-      const u32x4 end = row.partial(last);
-#pragma unroll
-      for (int n = 0; n < NC; ++n)
-        if (c0 + n * B == last) v[n] = end;
-    }
+  for (int n = 0; n < NC; ++n) request(row, tile * (B * NC) + n * B + tid, v[n]);
+}
+// The thread's index as a number that the compiler knows nothing of.  Taken anew for every row: what it can tell ahead of all rows (sixteen
+// offsets, sixteen comparisons' sides) it keeps in registers from row to row.
+__device__ __forceinline__ int thread_again(int tid) {
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
+// A chunk as a shift register: its first element, and the others moved down by one with another at the end.  (The rare paths go through
+// a chunk element by element in a loop: written out they would take registers from the common one.)
+template <typename S>
+__device__ __forceinline__ S shift_out(u32x4& v, S in) {
+  if constexpr (sizeof(S) == 4) {
+    const S first = __uint_as_float(v[0]);
+    v = u32x4{v[1], v[2], v[3], __float_as_uint(in)};
+    return first;
+  } else {
+    const S first = (S)v[0];
+    v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16),
+              __builtin_amdgcn_alignbit(v[3], v[2], 16), __builtin_amdgcn_alignbit((unsigned)in, v[3], 16)};
+    return first;
   }
 }
+
+// The row's first and last chunk cut to the row, in the two threads that hold them.
+template <typename S>
+__device__ __forceinline__ u32x4 cut(const Row<S>& row, int c, u32x4 v) {
+  const bool there = c >= row.first_load && c < row.end_load;
+#pragma unroll 1
+  for (int j = 0; j < Row<S>::N; ++j) {
+    S x = shift_out<S>(v, S(0));
+    if (!row.has(c, j)) x = Elements<S>::nothing();
+    else if (!there) x = row.at[c * Row<S>::N - row.lead + j];
+    if constexpr (sizeof(S) == 4) v[3] = __float_as_uint(x);
+    else v[3] = (v[3] & 0xffffu) | ((unsigned)x << 16);
+  }
+  return v;
+}
+template <typename S, int B>
+__device__ __forceinline__ void cut_ends(const Row<S>& row, int tile, int tid, u32x4 (&v)[NC]) {
+  const int c0 = tile * (B * NC) + tid, last = row.chunks - 1;
+  if (row.lead && c0 == 0) v[0] = cut(row, 0, v[0]);
+  if (!row.whole(last) && last >= c0 && last < c0 + B * NC && (last - c0) % B == 0 && !(row.lead && last == 0)) {
+    u32x4 end = neutral<S>();
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      if (c0 + n * B == last) end = v[n];
+    end = cut(row, last, end);
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      if (c0 + n * B == last) v[n] = end;
+  }
+}
+
+// A number that is the same in all lanes, moved to where it takes no register of theirs.
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 // Running maximum m of the elements seen, s = sum exp2((z - m) c) and (ENTROPY, c = log2 e) w = sum exp(z - m) (z - m).  32 bits:
 // sums of at most 2^28 terms in [0, 1], in groups of at most 2^20 per thread.
@@ -115,10 +172,34 @@ __device__ __forceinline__ float reference(float m) { return m == NEG_INF ? 0.f 
 // The sums of `a` taken over from its maximum to `m`, which is no smaller.
 template <bool ENTROPY>
 __device__ __forceinline__ Stats moved(const Stats& a, float m, float c) {
-  if (!(a.s > 0.f)) return Stats{m, 0.f, 0.f};               // nothing in it (or NaN, which m tells)
+  if (a.s == 0.f) return Stats{m, 0.f, 0.f};                 // nothing in it
   const float d = a.m - m, f = exp2_fast(d * c);
   // (a maximum far below: f is 0, and d can be -inf)
   return Stats{m, a.s * f, ENTROPY ? f * (a.w + a.s * fmaxf(d, -1000.f)) : 0.f};
+}
+
+// The largest element of a tile.  bf16: by the halves' bits as signed 16-bit numbers, two elements an instruction and none taken
+// apart, which is the numbers' order as soon as one of them is not negative; a thread with nothing but negative ones looks again.
+// (A NaN with its sign set is missed here.  Its exponential is NaN all the same, and so are the sums.)
+template <typename S, int B>
+__device__ __forceinline__ float largest(const u32x4 (&v)[NC], int chunks_left) {
+  constexpr int N = Elements<S>::N;
+  float m = NEG_INF;
+  if constexpr (sizeof(S) == 2) {
+    s16x2 top = {-32768, -32768};
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      if (n * B < chunks_left)                               // (the same for all threads)
+        top = __builtin_elementwise_max(top, top_halves(v[n]));
+    const short x = max(top[0], top[1]);
+    if (x >= 0) return __uint_as_float((unsigned)x << 16);
+  }
+#pragma unroll
+  for (int n = 0; n < NC; ++n)
+    if (n * B < chunks_left)
+#pragma unroll
+      for (int j = 0; j < N; j += 2) m = max_nan(m, max_nan(Elements<S>::get(v[n], j), Elements<S>::get(v[n], j + 1)));
+  return m;
 }
 
 // Before a tile is used again: its elements are taken apart anew then, instead of all of them being held taken apart in twice the
@@ -131,13 +212,7 @@ __device__ __forceinline__ void use_again(u32x4 (&v)[NC]) {
 template <typename S, int B, bool ENTROPY>
 __device__ __forceinline__ void add_tile(u32x4 (&v)[NC], int chunks_left, Stats& a, float c) {
   constexpr int N = Elements<S>::N;
-  float m = a.m;
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    if (n * B < chunks_left)                                 // (the same for all threads)
-#pragma unroll
-    for (int j = 0; j < N; j += 2) m = max_nan(m, max_nan(Elements<S>::get(v[n], j), Elements<S>::get(v[n], j + 1)));
-  }
+  const float m = max_nan(a.m, largest<S, B>(v, chunks_left));
   if (!(m == a.m)) a = moved<ENTROPY>(a, m, c);
   const float r = reference(m);
   use_again(v);
@@ -149,7 +224,7 @@ __device__ __forceinline__ void add_tile(u32x4 (&v)[NC], int chunks_left, Stats&
     for (int j = 0; j < N; ++j) {
       // the difference first: a masked logit may be the type's lowest value, whose product with log2 e overflows
       float d = Elements<S>::get(v[n], j) - r;
-      if (ENTROPY) d = fmaxf(d, -1000.f);                    // exp is 0 there, and 0 times -inf is not
+      if (ENTROPY) d = max_nan(d, -1000.f);                  // exp is 0 there, and 0 times -inf is not
       const float e = exp2_fast(d * c);
       s[j & 1] += e;
       if (ENTROPY) w[j & 1] = fmaf(e, d, w[j & 1]);
@@ -198,7 +273,7 @@ __device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(
 
 // ---- log probabilities ----------------------------------------------------------------------------
 struct LogprobArgs {
-  const void* logits; int64_t ld; int V;
+  const void* logits; int64_t ld, T; int V;
   const int64_t* tokens;
   int K;
   float* logprob; float* entropy; float* top_logprob; int32_t* top_ids;
@@ -263,85 +338,92 @@ __device__ void select_exactly(const S* z, int V, int K, SearchSpace<B>* q) {
   __syncthreads();
 }
 
-// The K best of a row.  Every thread knows the largest of its own elements; at least K of those are no smaller than the K-th largest
-// of them, which is therefore a threshold that the K best reach, and few others do (256 threads, K = 64: about 74 elements).  They are
-// collected in any order and sorted by counting, each against all; no two compare equal, so the result has one order.
+// The K best of a row.  Every thread knows the largest of the elements it has seen; at least K of those are no smaller than the K-th
+// largest of them, which is therefore a threshold that the K best reach, and few others do (256 threads, K = 64: about 74 elements of a
+// tile).  After every tile the threshold is found anew and the tile's elements that reach it are collected, in any order, while they are in
+// registers; what an earlier, lower threshold let in does no harm.  At the end the candidates are sorted by counting, each against all; no
+// two compare equal, so the result has one order.
+
+// The largest key that at least K of the threads' largest elements reach (bf16: to 16 bits, which is exact; more threads than 256 in fours,
+// since their number is what the search costs); 0 if they are fewer.
 template <typename S, int B>
-__device__ void best_of_row(const Row<S>& row, u32x4 (&held)[NC], int tiles, const LogprobArgs& p, const Stats& own, const Stats& all,
-                            int64_t t, SearchSpace<B>* q) {
-  constexpr int N = Elements<S>::N;
+__device__ __forceinline__ float find_threshold(float own, bool seen, int K, bool first, SearchSpace<B>* q) {
   const int tid = threadIdx.x, lane = tid & 63;
-  const float log_s = logf(all.s);
-  float* const out = p.top_logprob + t * p.K;
-  int32_t* const ids = p.top_ids + t * p.K;
-  if (!(all.m == all.m)) {                                   // NaN in the row: no order
-    for (int j = tid; j < p.K; j += B) { out[j] = all.m; ids[j] = j; }
-    return;
-  }
-  unsigned threshold;
-  if (p.K == 1) {
-    threshold = order_key(all.m);
-    if (tid == 0) q->count = 0;
-  } else {
-    q->key[tid] = tid < row.chunks ? order_key(own.m) : 0u;
-    if (tid == 0) q->count = 0;
-    __syncthreads();
-    if (tid < 64) {
-      constexpr int GROUPS = B >= 256 ? 4 : 1, EACH = B / (64 * GROUPS);
-      unsigned k[GROUPS];
+  q->key[tid] = seen ? order_key(own) : 0u;
+  __syncthreads();
+  if (tid < 64) {
+    constexpr int GROUPS = B >= 256 ? 4 : B / 64, EACH = B / (64 * GROUPS);
+    unsigned k[GROUPS];
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        k[g] = 0;
+    for (int g = 0; g < GROUPS; ++g) {
+      k[g] = 0;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) k[g] = max(k[g], q->key[(e * GROUPS + g) * 64 + lane]);
-      }
-      unsigned found = 0;                                    // the largest key that at least K groups reach, by its bits (bf16: the upper ones)
-      for (int b = 31; b >= (sizeof(S) == 2 ? 16 : 0); --b) {
-        const unsigned at = found | (1u << b);
-        int n = 0;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) n += __popcll(__ballot(k[g] >= at));
-        if (n >= p.K) found = at;
-      }
-      if (lane == 0) q->threshold = found;
+      for (int e = 0; e < EACH; ++e) k[g] = max(k[g], q->key[(e * GROUPS + g) * 64 + lane]);
     }
-    __syncthreads();
-    threshold = q->threshold;
-  }
-  // (fewer than K groups with elements: everything)
-  const float least = threshold <= 0x007fffffu ? NEG_INF : key_value(threshold);
-  if (p.K == 1) __syncthreads();                             // the count is 0
-  if (own.m >= least) {
-    auto collect = [&](const u32x4& v, int c) {
-      float m = NEG_INF;
+    unsigned found = 0;
+#pragma unroll 1
+    for (int b = 31; b >= (sizeof(S) == 2 ? 16 : 0); --b) {
+      const unsigned at = found | (1u << b);
+      int n = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j) m = fmaxf(m, Elements<S>::get(v, j));
-      if (m < least) return;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float z = Elements<S>::get(v, j);
-        const int i = c * N - row.lead + j;
-        if (z >= least && i >= 0 && i < row.V) {
-          const int at = atomicAdd(&q->count, 1);
-          if (at < CANDIDATES) q->candidate[at] = ((unsigned long long)order_key(z) << 32) | (unsigned)~i;
-        }
-      }
-    };
-    if (tiles == 1) {
-      use_again(held);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        if (n * B < row.chunks) collect(held[n], n * B + tid);
-      }
-    } else {
-      for (int c = tid; c < row.chunks; c += B)
-        collect(row.whole(c) ? *(const u32x4*)(row.at + ((int64_t)c * N - row.lead)) : row.partial(c), c);
+      for (int g = 0; g < GROUPS; ++g) n += __popcll(__ballot(k[g] >= at));
+      if (n >= K) found = at;
+    }
+    if (lane == 0) {
+      q->threshold = found;
+      if (first) q->count = 0;
     }
   }
   __syncthreads();
+  const unsigned threshold = q->threshold;
+  return threshold <= 0x007fffffu ? NEG_INF : key_value(threshold);     // (too few: everything)
+}
+
+// The elements of a tile that reach `least`.
+template <typename S, int B>
+__device__ __forceinline__ void collect(const Row<S>& row, const u32x4 (&v)[NC], int tile, int tid, float least, SearchSpace<B>* q) {
+  constexpr int N = Elements<S>::N;
+  const int c0 = tile * (B * NC);
+#pragma unroll
+  for (int n = 0; n < NC; ++n)
+    if (c0 + n * B < row.chunks) {                           // (the same for all threads)
+      bool some;
+      if (sizeof(S) == 2 && least > 0.f) {                   // (the same for all threads; bits of positive numbers are in their order)
+        const s16x2 top = top_halves(v[n]);
+        some = max(top[0], top[1]) >= (short)(__float_as_uint(least) >> 16);
+      } else {
+        float m = Elements<S>::get(v[n], 0);
+#pragma unroll
+        for (int j = 1; j < N; ++j) m = fmaxf(m, Elements<S>::get(v[n], j));
+        some = m >= least;
+      }
+      if (some) {
+        const int i0 = (c0 + n * B + tid) * N - row.lead;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float z = Elements<S>::get(v[n], j);
+          if (z >= least && i0 + j >= 0 && i0 + j < row.V) {
+            const int at = atomicAdd(&q->count, 1);
+            if (at < CANDIDATES) q->candidate[at] = ((unsigned long long)order_key(z) << 32) | (unsigned)~(i0 + j);
+          }
+        }
+      }
+    }
+}
+
+template <typename S, int B>
+__device__ __forceinline__ void write_best(const S* row, const LogprobArgs& p, const Stats& all, int64_t t, SearchSpace<B>* q) {
+  const int tid = threadIdx.x;
+  const float log_s = logf(all.s);
+  float* const out = p.top_logprob + t * p.K;
+  int32_t* const ids = p.top_ids + t * p.K;
+  if (!(all.s == all.s)) {                                   // NaN or +inf in the row: no order
+    for (int j = tid; j < p.K; j += B) { out[j] = all.s; ids[j] = j; }
+    return;
+  }
   if (q->count > CANDIDATES) {                               // (the same for all threads)
     __syncthreads();
-    select_exactly<S, B>(row.at, row.V, p.K, q);
+    select_exactly<S, B>(row, p.V, p.K, q);
   }
   const int n = q->count;
   for (int i = tid; i < n; i += B) {
@@ -360,33 +442,43 @@ template <typename S, int B>
 __global__ __launch_bounds__(B) void token_logprobs_kernel(LogprobArgs p) {
   __shared__ float shared[3 * (B / 64)];
   __shared__ SearchSpace<B> search;
+  int tid = threadIdx.x;
   const int64_t t = blockIdx.x;
-  const Row<S> row((const S*)p.logits + t * p.ld, p.V);
-  const int tiles = (row.chunks + B * NC - 1) / (B * NC);
+  const Row<S> row(p.logits, p.ld, p.V, t, p.T);
+  const int64_t y = p.tokens[t];
   u32x4 v[NC];
   Stats own = {NEG_INF, 0.f, 0.f};
-  for (int i = 0; i < tiles; ++i) {
-    load_tile<S, B>(row, i, v);
-    add_tile<S, B, true>(v, row.chunks - i * (B * NC), own, LOG2E);
+  for (int tile = 0; tile * (B * NC) < row.chunks; ++tile) {
+    tid = thread_again(tid);
+    request_tile<S, B>(row, tile, tid, v);
+    cut_ends<S, B>(row, tile, tid, v);
+    add_tile<S, B, true>(v, row.chunks - tile * (B * NC), own, LOG2E);
+    if (p.K > 0) {
+      const float least = find_threshold<S, B>(own.m, tid < row.chunks, p.K, tile == 0, &search);
+      use_again(v);
+      collect<S, B>(row, v, tile, tid, least, &search);
+    }
   }
   const Stats all = join<B, true>(own, LOG2E, shared);
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     const float log_s = logf(all.s);
-    const int64_t y = p.tokens[t];
     float lp = 0.f;                                          // no token given
     if (y >= p.V) lp = __builtin_nanf("");
     else if (y >= 0) lp = all.m == NEG_INF ? NEG_INF : (Elements<S>::load(row.at + y) - all.m) - log_s;
     p.logprob[t] = lp;
-    p.entropy[t] = all.m == NEG_INF ? 0.f : fmaxf(log_s - all.w / all.s, 0.f) + 0.f * all.m;   // (NaN and inf of m stay)
+    p.entropy[t] = all.m == NEG_INF ? 0.f : max_nan(log_s - all.w / all.s, 0.f);
   }
-  if (p.K > 0) best_of_row<S, B>(row, v, tiles, p, own, all, t, &search);
+  if (p.K > 0) {
+    if (B == 64) __syncthreads();                            // (more wavefronts met in join)
+    write_best<S, B>(row.at, p, all, t, &search);
+  }
 }
 
 // ---- distillation ---------------------------------------------------------------------------------
 enum DistillMode { LOSS = 0, LOSS_AND_GRADIENT = 1, GRADIENT = 2 };
 
 struct DistillArgs {
-  const void* logits; int64_t ld; int V;
+  const void* logits; int64_t ld, T; int V;
   const int32_t* ids; const float* teacher; int K;
   float tau;
   const float* weights;                      // LOSS*: optional; GRADIENT: the upstream gradient of each row's loss
@@ -395,124 +487,170 @@ struct DistillArgs {
 };
 
 constexpr int MAX_K = 128;                   // two entries per lane of the first wavefront
-struct Teacher { int id[MAX_K]; float q[MAX_K]; };
 
-// One wavefront, entries lane and lane + 64: q, the first of several entries with one id carrying their sum in `total`.
-struct Entry { int id; float z, q, log_q, total; bool first; };
+// A row's alternatives as they are in memory: entries lane and lane + 64 of the first wavefront.
+struct Alternatives {
+  int id[2];
+  float x[2];
+};
+__device__ __forceinline__ Alternatives request_alternatives(const DistillArgs& p, int64_t t) {
+  Alternatives a = {{-1, -1}, {NEG_INF, NEG_INF}};
+  if (t < p.T && threadIdx.x < 64)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j = threadIdx.x + 64 * h;
+      if (j < p.K) { a.id[h] = p.ids[t * p.K + j]; a.x[h] = p.teacher[t * p.K + j]; }
+    }
+  return a;
+}
 
-template <typename S>
-__device__ __forceinline__ bool read_teacher(const DistillArgs& p, const Row<S>& row, int64_t t, Teacher* shared, Entry (&e)[2]) {
+// What the first wavefront keeps of them while the row is worked on, out of the way of the registers: the id (-1: not there), q, log q, the
+// student's logit, and for the first of the entries with one id (ids are all different as a rule) the sum of their q, else -1.
+struct __attribute__((aligned(16))) Teacher { int id[MAX_K]; float q[MAX_K], log_q[MAX_K], z[MAX_K], total[MAX_K]; };
+
+// Entries and weights of a row into LDS; whether there is any.  One wavefront.
+__device__ __forceinline__ bool weigh(const DistillArgs& p, const Alternatives& a, Teacher* e) {
   const int lane = threadIdx.x & 63;
   const float c = LOG2E / p.tau;
-  float x[2], m = NEG_INF;
+  float q[2], m = NEG_INF;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int j = lane + 64 * h;
-    e[h].id = -1; x[h] = NEG_INF; e[h].z = 0.f;
-    if (j < p.K) { e[h].id = p.ids[t * p.K + j]; x[h] = p.teacher[t * p.K + j]; }
-    if (e[h].id < 0 || e[h].id >= row.V || x[h] == NEG_INF) { e[h].id = -1; x[h] = NEG_INF; }
-    if (e[h].id >= 0) e[h].z = Elements<S>::load(row.at + e[h].id);
-    m = max_nan(m, x[h]);
-  }
+  for (int h = 0; h < 2; ++h)
+    if (a.id[h] >= 0) m = max_nan(m, a.x[h]);
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = max_nan(m, __shfl_xor(m, o));
-  if (m == NEG_INF) return false;                            // no alternative is there
+  const float r = reference(m);                              // (no alternative is there: everything below is 0)
   float s = 0.f;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) { e[h].q = exp2_fast((x[h] - m) * c); s += e[h].q; }
+  for (int h = 0; h < 2; ++h) { q[h] = a.id[h] >= 0 ? exp2_fast((a.x[h] - r) * c) : 0.f; s += q[h]; }
 #pragma unroll
   for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
   const float log_s = logf(s);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    e[h].q /= s;
-    e[h].log_q = (x[h] - m) / p.tau - log_s;
     const int j = lane + 64 * h;
-    shared->id[j] = e[h].id; shared->q[j] = e[h].q;
-    e[h].total = 0.f; e[h].first = e[h].id >= 0;
+    q[h] /= s;
+    e->id[j] = a.id[h]; e->q[j] = q[h]; e->log_q[j] = (a.x[h] - r) / p.tau - log_s;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  for (int j = 0; j < p.K; ++j) {
-    const int id = shared->id[j];
-    const float q = shared->q[j];
+  // Is an id there twice?  (Entries that are not there have ids of their own, so that they are not found alike.)
+  int mine[2], found[2] = {0, 0};
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (id == e[h].id) {
-        e[h].total += q;
-        if (j < lane + 64 * h) e[h].first = false;
-      }
+  for (int h = 0; h < 2; ++h) mine[h] = a.id[h] >= 0 ? a.id[h] : -2 - (lane + 64 * h);
+  const bool many = p.K > 64;
+#pragma unroll 4
+  for (int j = 0; j < p.K; j += 4) {
+    const i32x4 id = *(const i32x4*)(e->id + j);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      found[0] += id[k] == mine[0];
+      if (many) found[1] += id[k] == mine[1];
+    }
   }
-  return true;
+  float total[2] = {q[0], q[1]};
+  bool first[2] = {a.id[0] >= 0, a.id[1] >= 0};
+  if (__ballot(found[0] > 1 || found[1] > 1)) {
+    total[0] = total[1] = 0.f;
+    for (int j = 0; j < p.K; ++j) {
+      const int id = e->id[j];
+      const float qj = e->q[j];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (id == a.id[h]) {
+          total[h] += qj;
+          if (j < lane + 64 * h) first[h] = false;
+        }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) e->total[lane + 64 * h] = first[h] ? total[h] : -1.f;
+  return !(m == NEG_INF);
 }
 
-template <typename S, int B>
-__device__ __forceinline__ void store_chunk(const Row<S>& row, S* out, bool aligned, int c, const u32x4& v) {
-  constexpr int N = Elements<S>::N;
-  const int i0 = c * N - row.lead;
+template <typename S>
+__device__ __forceinline__ void store_chunk(const Row<S>& row, S* out, bool aligned, int c, u32x4 v) {
+  const int i0 = c * Row<S>::N - row.lead;
   if (aligned && row.whole(c)) {
     *(u32x4*)(out + i0) = v;
     return;
   }
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const S x = sizeof(S) == 4 ? __builtin_bit_cast(S, (typename std::conditional<sizeof(S) == 4, unsigned, uint16_t>::type)v[sizeof(S) == 4 ? j : 0])
-                               : __builtin_bit_cast(S, (typename std::conditional<sizeof(S) == 4, unsigned, uint16_t>::type)(v[j >> 1] >> (16 * (j & 1))));
-    if (i0 + j >= 0 && i0 + j < row.V) out[i0 + j] = x;
+#pragma unroll 1
+  for (int j = 0; j < Row<S>::N; ++j) {
+    const S x = shift_out<S>(v, S(0));
+    if (row.has(c, j)) out[i0 + j] = x;
   }
 }
 
-template <typename S, int B, int MODE>
+// HELD: the row fits the workgroup's registers.
+template <typename S, int B, int MODE, bool HELD>
 __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
   constexpr int N = Elements<S>::N;
   __shared__ float shared[3 * (B / 64)];
   __shared__ Teacher teacher;
   __shared__ int present;
-  const int tid = threadIdx.x;
+  int tid = threadIdx.x;
   const int64_t t = blockIdx.x;
-  const Row<S> row((const S*)p.logits + t * p.ld, p.V);
-  const int tiles = (row.chunks + B * NC - 1) / (B * NC);
+  const Row<S> row(p.logits, p.ld, p.V, t, p.T);
+  const int tiles = HELD ? 1 : (row.chunks + B * NC - 1) / (B * NC);
   S* const out = MODE == LOSS ? nullptr : (S*)p.grad + t * p.ld_grad;
   const bool aligned = (((uintptr_t)out ^ (uintptr_t)row.at) & 15) == 0;
-  const float weight = p.weights ? p.weights[t] : 1.f;
+  const float weight = p.weights ? uniform(p.weights[t]) : 1.f;
   auto write_zeros = [&]() {
-    for (int c = tid; c < row.chunks; c += B) store_chunk<S, B>(row, out, aligned, c, u32x4{0, 0, 0, 0});
+    for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0});
   };
   if (weight == 0.f) {                                       // the row is left out: its logits are not read
     if (MODE != GRADIENT && tid == 0) { p.loss[t] = 0.f; p.stats[2 * t] = 0.f; p.stats[2 * t + 1] = 0.f; }
     if (MODE != LOSS) write_zeros();
     return;
   }
-  const float c = LOG2E / p.tau;
+  const float c = uniform(LOG2E / p.tau);
+  Alternatives alt = request_alternatives(p, t);             // (in front of the row's chunks: loads return in order)
   u32x4 v[NC];
-  if (tiles == 1) load_tile<S, B>(row, 0, v);                // (on its way while the teacher's entries are read)
-  Entry e[2];
+  if (HELD) request_tile<S, B>(row, 0, tid, v);
+  float z[2];
   if (tid < 64) {
-    const bool any = read_teacher<S>(p, row, t, &teacher, e);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (alt.id[h] >= p.V || alt.x[h] == NEG_INF) alt.id[h] = -1;             // not there
+      z[h] = alt.id[h] >= 0 ? Elements<S>::load(row.at + alt.id[h]) : 0.f;
+    }
+    const bool any = weigh(p, alt, &teacher);
     if (tid == 0) present = any;
-    asm volatile("" :: "v"(e[0].z), "v"(e[1].z));            // (they are here: grad may be the logits' own memory)
   }
+  // (they are here before anybody writes: grad may be the logits' own memory)
+  auto keep_logits = [&]() {
+    if (tid < 64)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) teacher.z[tid + 64 * h] = z[h];
+  };
   float m, log_s, inv_s = 1.f;
   if (MODE != GRADIENT) {
     Stats all = {NEG_INF, 0.f, 0.f};
     for (int i = 0; i < tiles; ++i) {
-      if (tiles > 1) load_tile<S, B>(row, i, v);
+      tid = thread_again(tid);
+      if (!HELD) request_tile<S, B>(row, i, tid, v);
+      cut_ends<S, B>(row, i, tid, v);
       add_tile<S, B, false>(v, row.chunks - i * (B * NC), all, c);
     }
+    keep_logits();
     all = join<B, false>(all, c, shared);
-    m = all.m; log_s = logf(all.s); inv_s = 1.f / all.s;
+    m = uniform(all.m); log_s = uniform(logf(all.s)); inv_s = uniform(1.f / all.s);
   } else {
-    m = p.stats[2 * t]; log_s = p.stats[2 * t + 1];
+    m = uniform(p.stats[2 * t]); log_s = uniform(p.stats[2 * t + 1]);
+    keep_logits();
   }
-  __syncthreads();
+  if (MODE == GRADIENT || B == 64) __syncthreads();          // `present` is there (more wavefronts met in join)
   // No alternative, or no logit above -inf: nothing to learn from.
-  const bool nothing = !present || m == NEG_INF;
+  const bool nothing = !__builtin_amdgcn_readfirstlane(present) || m == NEG_INF;
   if (MODE != GRADIENT && tid < 64) {
     float x = 0.f;
     if (!nothing)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (e[h].id >= 0 && !(e[h].q == 0.f)) x += e[h].q * (e[h].log_q - ((e[h].z - m) / p.tau - log_s));
+      for (int h = 0; h < 2; ++h) {
+        const int j = tid + 64 * h;
+        const float q = teacher.q[j];
+        if (teacher.id[j] >= 0 && !(q == 0.f)) x += q * (teacher.log_q[j] - ((teacher.z[j] - m) / p.tau - log_s));
+      }
 #pragma unroll
     for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
     if (tid == 0) {
@@ -527,42 +665,73 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
     return;
   }
   // p_i = exp((z_i - m) / tau) / s, the division (GRADIENT: an exponent) once per row
-  const float scale = weight * p.tau, shift = MODE == GRADIENT ? -log_s * LOG2E : 0.f;
-  const float factor = MODE == GRADIENT ? scale : scale * inv_s;
+  const float scale = uniform(weight * p.tau), shift = MODE == GRADIENT ? uniform(-log_s * LOG2E) : 0.f;
+  const float factor = uniform(scale * inv_s);
   for (int i = 0; i < tiles; ++i) {
-    if (tiles > 1) load_tile<S, B>(row, i, v);
+    tid = thread_again(tid);
+    if (!HELD) request_tile<S, B>(row, i, tid, v);
+    if (!HELD || MODE == GRADIENT) cut_ends<S, B>(row, i, tid, v);
     else use_again(v);
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      const int at = i * (B * NC) + n * B;
-      if (at + tid < row.chunks) {
+      const int at = i * (B * NC) + n * B + tid;
+      if (at < row.chunks) {
         float x[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float d = Elements<S>::get(v[n], j) - m;
           x[j] = factor * exp2_fast(MODE == GRADIENT ? fmaf(d, c, shift) : d * c);
         }
-        store_chunk<S, B>(row, out, aligned, at + tid, Elements<S>::pack(x));
+        store_chunk(row, out, aligned, at, Elements<S>::pack(x));
       }
     }
   }
   __syncthreads();                                           // the row is written: the teacher's entries go over it
   if (tid < 64)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (e[h].first) {
-        const float d = e[h].z - m;
+    for (int h = 0; h < 2; ++h) {
+      const int j = tid + 64 * h, id = teacher.id[j];
+      const float total = teacher.total[j];
+      if (id >= 0 && !(total == -1.f)) {
+        const float d = teacher.z[j] - m;
         const float pz = MODE == GRADIENT ? exp2_fast(fmaf(d, c, shift)) : exp2_fast(d * c) * inv_s;
-        Elements<S>::store(out + e[h].id, scale * (pz - e[h].total));
+        Elements<S>::store(out + id, scale * (pz - total));
       }
+    }
 }
 
-// Threads per row.  A row of up to 16 chunks per thread of one wavefront needs no barrier; few rows get 1024 threads, since
-// there is nothing else for the compute units to do.
-int threads_per_row(int64_t T, int V, moep_dtype dt) {
-  const int64_t chunks = ceil_div((int64_t)V * (int64_t)dtype_size(dt), 16) + 1;
+// Threads per row of a loss: the fewest whose registers hold it whole, so that many rows are in flight on a compute unit at different
+// points of their way, and fewer barriers stop them; few rows get more threads, since there is nothing else for the compute units to
+// do.  0: none hold it.
+int threads_to_hold(int64_t T, int64_t chunks) {
+  if (chunks > 1024 * NC) return 0;
   if (T <= 512 && chunks > 256) return 1024;
-  return chunks <= 512 && T > 2048 ? 64 : 256;
+  for (int b : {64, 128, 256, 512})
+    if (chunks <= b * NC) return b;
+  return 1024;
+}
+// Threads per row of log probabilities, which need not be held: one wavefront where that holds the row, else 256, of few rows more.
+int threads_to_read(int64_t T, int64_t chunks) {
+  if (chunks <= 64 * NC && T > 2048) return 64;
+  for (int b : {256, 512})
+    if (T * b >= 150000 || chunks <= b) return b;
+  return 1024;
+}
+// Chunks of a row at most: its elements from the 16-byte boundary before it on, which is as far for every row where `ld` is whole chunks.
+int64_t most_chunks(const void* logits, int64_t ld, int64_t V, moep_dtype dt) {
+  const int64_t size = (int64_t)dtype_size(dt), n = 16 / size;
+  return ceil_div(V + (ld % n ? n - 1 : (int64_t)((uintptr_t)logits & 15) / size), n);
+}
+
+template <typename F>
+void with_threads(int threads, F launch) {
+  switch (threads) {
+    case 64: launch(std::integral_constant<int, 64>{}); break;
+    case 128: launch(std::integral_constant<int, 128>{}); break;
+    case 256: launch(std::integral_constant<int, 256>{}); break;
+    case 512: launch(std::integral_constant<int, 512>{}); break;
+    default: launch(std::integral_constant<int, 1024>{});
+  }
 }
 
 int check_rows(const char* who, int64_t T, int64_t V, moep_dtype dt, const void* logits, int64_t ld) {
@@ -576,19 +745,17 @@ int check_rows(const char* who, int64_t T, int64_t V, moep_dtype dt, const void*
 
 template <int MODE>
 int launch_distill(const DistillArgs& p, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
-  const int threads = threads_per_row(T, p.V, dt);
+  const int64_t chunks = most_chunks(p.logits, p.ld, p.V, dt);
+  const int threads = threads_to_hold(T, chunks);
   Timed timed(name, s);
-#define MOEP_DISTILL(S, B) hipLaunchKernelGGL((distill_topk_kernel<S, B, MODE>), dim3((unsigned)T), dim3(B), 0, s, p)
-  if (dt == MOEP_BF16) {
-    if (threads == 64) MOEP_DISTILL(uint16_t, 64);
-    else if (threads == 256) MOEP_DISTILL(uint16_t, 256);
-    else MOEP_DISTILL(uint16_t, 1024);
-  } else {
-    if (threads == 64) MOEP_DISTILL(float, 64);
-    else if (threads == 256) MOEP_DISTILL(float, 256);
-    else MOEP_DISTILL(float, 1024);
-  }
-#undef MOEP_DISTILL
+  auto with = [&](auto b, auto held) {
+    constexpr int B = decltype(b)::value;
+    constexpr bool HELD = decltype(held)::value;
+    if (dt == MOEP_BF16) hipLaunchKernelGGL((distill_topk_kernel<uint16_t, B, MODE, HELD>), dim3((unsigned)T), dim3(B), 0, s, p);
+    else hipLaunchKernelGGL((distill_topk_kernel<float, B, MODE, HELD>), dim3((unsigned)T), dim3(B), 0, s, p);
+  };
+  if (threads) with_threads(threads, [&](auto b) { with(b, std::true_type{}); });
+  else with(std::integral_constant<int, 512>{}, std::false_type{});
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
@@ -615,22 +782,16 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
   if (T == 0) return MOEP_OK;
   if (!logits || !tokens || !logprob || !entropy) return fail(MOEP_EINVAL, "%s: NULL logits, tokens, logprob or entropy", who);
   if (K > 0 && (!top_logprob || !top_ids)) return fail(MOEP_EINVAL, "%s: NULL top_logprob or top_ids", who);
-  LogprobArgs p = {logits, ld, (int)V, tokens, K, logprob, entropy, top_logprob, top_ids};
+  LogprobArgs p = {logits, ld, T, (int)V, tokens, K, logprob, entropy, top_logprob, top_ids};
   hipStream_t s = (hipStream_t)hip_stream;
-  int threads = threads_per_row(T, p.V, dt);
-  if (threads == 64 && K > 32) threads = 256;                // (a threshold from 64 groups would let too many through)
+  int threads = threads_to_read(T, most_chunks(logits, ld, V, dt));
+  while (threads < 256 && 2 * K > threads) threads *= 2;     // (a threshold from few more than K threads lets too many through)
   Timed timed("token_logprobs", s);
-#define MOEP_LOGPROBS(S, B) hipLaunchKernelGGL((token_logprobs_kernel<S, B>), dim3((unsigned)T), dim3(B), 0, s, p)
-  if (dt == MOEP_BF16) {
-    if (threads == 64) MOEP_LOGPROBS(uint16_t, 64);
-    else if (threads == 256) MOEP_LOGPROBS(uint16_t, 256);
-    else MOEP_LOGPROBS(uint16_t, 1024);
-  } else {
-    if (threads == 64) MOEP_LOGPROBS(float, 64);
-    else if (threads == 256) MOEP_LOGPROBS(float, 256);
-    else MOEP_LOGPROBS(float, 1024);
-  }
-#undef MOEP_LOGPROBS
+  with_threads(threads, [&](auto b) {
+    constexpr int B = decltype(b)::value;
+    if (dt == MOEP_BF16) hipLaunchKernelGGL((token_logprobs_kernel<uint16_t, B>), dim3((unsigned)T), dim3(B), 0, s, p);
+    else hipLaunchKernelGGL((token_logprobs_kernel<float, B>), dim3((unsigned)T), dim3(B), 0, s, p);
+  });
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
@@ -645,7 +806,7 @@ int moe_distill_topk(const void* logits, int64_t ld, const int32_t* ids, const f
     if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
   if (T == 0) return MOEP_OK;
   if (!logits || !loss || !stats) return fail(MOEP_EINVAL, "%s: NULL logits, loss or stats", who);
-  DistillArgs p = {logits, ld, (int)V, ids, teacher, K, temperature, weights, loss, stats, grad, ld_grad};
+  DistillArgs p = {logits, ld, T, (int)V, ids, teacher, K, temperature, weights, loss, stats, grad, ld_grad};
   return grad ? launch_distill<LOSS_AND_GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "distill_loss_gradient")
               : launch_distill<LOSS>(p, T, dt, (hipStream_t)hip_stream, "distill_loss");
 }
@@ -659,7 +820,7 @@ int moe_distill_topk_backward(const void* logits, int64_t ld, const int32_t* ids
   if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
   if (T == 0) return MOEP_OK;
   if (!logits || !stats || !grad_loss || !grad) return fail(MOEP_EINVAL, "%s: NULL logits, stats, grad_loss or grad", who);
-  DistillArgs p = {logits, ld, (int)V, ids, teacher, K, temperature, grad_loss, nullptr, (float*)stats, grad, ld_grad};
+  DistillArgs p = {logits, ld, T, (int)V, ids, teacher, K, temperature, grad_loss, nullptr, (float*)stats, grad, ld_grad};
   return launch_distill<GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "distill_gradient");
 }
 
