@@ -425,10 +425,12 @@ static int multiply_f32_out(const Product& q, moep_dtype dt, float* out, hipStre
   g.M = q.M; g.N = q.N; g.K = kc; g.experts = q.ranges; g.epilogue = EPI_STORE;
   return launch_gemm_f32(g, s, name);
 }
-static int multiply(const Product& q, moep_dtype dt, void* C, float* part, hipStream_t s, const char* name) {
+// The sums of a product in several ranges are left to the caller: `sums` gets what launch_sums has to do, `n_sums` counts it.
+static int multiply(const Product& q, moep_dtype dt, void* C, float* part, SumJob* sums, int* n_sums, hipStream_t s, const char* name) {
   if (q.ranges > 1) {
-    if (int st = multiply_f32_out(q, dt, part, s, name)) return st;
-    return launch_sum_parts(part, q.ranges, q.M * q.N, q.M * q.N, dt, C, s);
+    SumJob& sum = sums[(*n_sums)++];
+    sum.part = part; sum.parts = q.ranges; sum.stride = sum.n = q.M * q.N; sum.out = C;
+    return multiply_f32_out(q, dt, part, s, name);
   }
   if (dt == MOEP_F32) return multiply_f32_out(q, dt, (float*)C, s, name);
   PackedGemmArgs g;
@@ -500,7 +502,10 @@ int expert_ffn_forward(const void* x, const void* W1, const void* W3, const void
     if (int st = launch_gemm_f32(up, s, "ffn_gate_up")) return st;
   }
   const Product down = {h, W2, true, T, H, F, ranges_of(T, H, F, dt, false)};
-  return multiply(down, dt, y, (float*)rest, s, "ffn_down");
+  SumJob sum[1];
+  int n_sums = 0;
+  if (int st = multiply(down, dt, y, (float*)rest, sum, &n_sums, s, "ffn_down")) return st;
+  return launch_sums(sum, n_sums, dt, s);
 }
 
 // The backward call's workspace.  `t_parts` ranges along the tokens for dW2, half as many (where even) for dW1 and dW3, which have
@@ -571,12 +576,28 @@ int expert_ffn_backward(const void* dy, const void* x, const void* W1, const voi
   const Operand none;
 
   const Operand w2t = operand(p.w2t, F, H, true), dy_a = operand(p.dy, T, H, false), dy_t = operand(p.dy_t, H, p.Tp, false);
-  if (int st = launch_transpose(W2, H, F, dt, w2t, 0, H, nullptr, s, "transpose_w")) return st;
+  const Operand w13t = operand(p.w13t, H, 2 * (int64_t)F, true), x_t = operand(p.x_t, H, p.Tp, true);
+  // every operand that is there already, transposed in one launch
+  TransposeJob jobs[MAX_JOBS];
+  int n_jobs = 0;
+  auto transpose = [&](const void* X, int64_t R, int C, const Operand& out, int64_t k0, int64_t k_end) -> TransposeJob& {
+    TransposeJob& j = jobs[n_jobs++];
+    j.X = X; j.R = R; j.C = C; j.out = out; j.k0 = k0; j.k_end = k_end;
+    return j;
+  };
+  transpose(W2, H, F, w2t, 0, H);
+  if (dx) {
+    transpose(W1, F, H, w13t, 0, F);
+    transpose(W3, F, H, w13t, F, 2 * (int64_t)F);
+  }
   if (weights) {
-    if (int st = launch_transpose(dy, T, H, dt, dy_t, 0, p.Tp, bf16 ? &dy_a : nullptr, s, "transpose_tokens")) return st;
+    transpose(x, T, H, x_t, 0, p.Tp);
+    TransposeJob& j = transpose(dy, T, H, dy_t, 0, p.Tp);
+    if (bf16) j.straight = dy_a;
   } else if (bf16) {
     if (int st = launch_pack_a_bf16(dy, H, T, H, dy_a.p, s, "pack_dy")) return st;
   }
+  if (int st = launch_transposes(jobs, n_jobs, dt, s)) return st;
   float* const dh = (float*)(at + p.dh);
   const Product q_dh = {bf16 ? dy_a.p : dy, w2t.p, false, T, F, H, p.dh_parts};
   if (int st = multiply_f32_out(q_dh, dt, dh, s, "ffn_dh")) return st;
@@ -585,22 +606,22 @@ int expert_ffn_backward(const void* dy, const void* x, const void* W1, const voi
                 db_t = operand(p.dadb_t + operand_bytes(p.rows13 / 2, p.Tp, dt), F, p.Tp, false), h_t = operand(p.h_t, F, p.Tp, true);
   if (int st = launch_gradients_of_branches(dh, p.dh_parts, gate_up, gate_up + T * F, T, F, dt, dx ? dab : none, weights ? da_t : none,
                                             weights ? db_t : none, weights ? h_t : none, s)) return st;
+  SumJob sums[MAX_JOBS];
+  int n_sums = 0;
   if (dx) {
-    const Operand w13t = operand(p.w13t, H, 2 * (int64_t)F, true);
-    if (int st = launch_transpose(W1, F, H, dt, w13t, 0, F, nullptr, s, "transpose_w")) return st;
-    if (int st = launch_transpose(W3, F, H, dt, w13t, F, 2 * (int64_t)F, nullptr, s, "transpose_w")) return st;
     const Product q = {dab.p, w13t.p, false, T, H, 2 * F, p.dx_parts};
-    if (int st = multiply(q, dt, dx, (float*)(at + p.dx_part), s, "ffn_dx")) return st;
+    if (int st = multiply(q, dt, dx, (float*)(at + p.dx_part), sums, &n_sums, s, "ffn_dx")) return st;
   }
-  if (!weights) return MOEP_OK;
-  const Operand x_t = operand(p.x_t, H, p.Tp, true);
-  if (int st = launch_transpose(x, T, H, dt, x_t, 0, p.Tp, nullptr, s, "transpose_tokens")) return st;
+  if (!weights) return launch_sums(sums, n_sums, dt, s);
   if (p.t_parts13 > 1) {                          // da^T over db^T as one operand: one launch, and a sum each
     float* const part = (float*)(at + p.w13_part);
     const Product q = {da_t.p, x_t.p, false, p.rows13, H, (int)p.Tp, p.t_parts13};
     if (int st = multiply_f32_out(q, dt, part, s, "ffn_dw13")) return st;
-    if (int st = launch_sum_parts(part, q.ranges, q.M * H, (int64_t)F * H, dt, dW1, s)) return st;
-    if (int st = launch_sum_parts(part + p.rows13 / 2 * H, q.ranges, q.M * H, (int64_t)F * H, dt, dW3, s)) return st;
+    for (int half = 0; half < 2; ++half) {
+      SumJob& sum = sums[n_sums++];
+      sum.part = part + half * (p.rows13 / 2) * H; sum.parts = q.ranges; sum.stride = q.M * H; sum.n = (int64_t)F * H;
+      sum.out = half ? dW3 : dW1;
+    }
   } else if (bf16) {
     PackedGemmArgs g;
     g.A = da_t.p; g.a_expert_bytes = db_t.p - da_t.p; g.B = x_t.p; g.b_shared = true;
@@ -615,7 +636,8 @@ int expert_ffn_backward(const void* dy, const void* x, const void* W1, const voi
     if (int st = launch_gemm_f32(g, s, "ffn_dw13")) return st;
   }
   const Product q = {dy_t.p, h_t.p, false, H, F, (int)p.Tp, p.t_parts};
-  return multiply(q, dt, dW2, (float*)(at + p.w2_part), s, "ffn_dw2");
+  if (int st = multiply(q, dt, dW2, (float*)(at + p.w2_part), sums, &n_sums, s, "ffn_dw2")) return st;
+  return launch_sums(sums, n_sums, dt, s);
 }
 
 // ------------------------------------------------------------------ prune_enumerate

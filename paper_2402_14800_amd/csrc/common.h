@@ -315,16 +315,30 @@ struct Operand {
 };
 size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt);
 // X [R, C] transposed into columns k0 .. of `out` (rows C, K at least k0 + R; columns k0 + R .. k_end - 1 are cleared); `straight`
-// (bf16, may be NULL): X itself as an operand of R rows as well.
-int launch_transpose(const void* X, int64_t R, int C, moep_dtype dt, const Operand& out, int64_t k0, int64_t k_end, const Operand* straight,
-                     hipStream_t s, const char* name);
+// (bf16, p may be NULL): X itself as an operand of R rows as well.  Several of them in one launch.
+struct TransposeJob {
+  const void* X = nullptr;
+  int64_t R = 0;
+  int C = 0;
+  Operand out;
+  int64_t k0 = 0, k_end = 0;
+  Operand straight;
+};
+constexpr int MAX_JOBS = 5;
+int launch_transposes(const TransposeJob* jobs, int n, moep_dtype dt, hipStream_t s);
 // From dh [parts, T, F] fp32 (to be summed) and the branches g, u [T, F] fp32: da and db as one operand [T, 2 F], and da, db and
 // h = silu(g) u transposed, [F, K] each, K >= T with zeros beyond T.
 int launch_gradients_of_branches(const float* dh, int parts, const float* g, const float* u, int64_t T, int F, moep_dtype dt, const Operand& dab,
                                  const Operand& da_t, const Operand& db_t, const Operand& h_t, hipStream_t s);
 int launch_silu_product(const float* g, const float* u, int64_t n, float* h, hipStream_t s);
-// out[i] = sum over parts of part[p * stride + i], i < n, in that order
-int launch_sum_parts(const float* part, int parts, int64_t stride, int64_t n, moep_dtype dt, void* out, hipStream_t s);
+// out[i] = sum over parts of part[p * stride + i], i < n, in that order.  Several of them in one launch.
+struct SumJob {
+  const float* part = nullptr;
+  int parts = 0;
+  int64_t stride = 0, n = 0;
+  void* out = nullptr;
+};
+int launch_sums(const SumJob* jobs, int n, moep_dtype dt, hipStream_t s);
 int launch_clear(void* p, size_t bytes, hipStream_t s);   // (bytes: a multiple of 16)
 
 // Host-side subset helpers (also used to fill the device mask table).

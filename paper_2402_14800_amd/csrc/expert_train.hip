@@ -53,40 +53,56 @@ template <typename S>
 struct Place {
   int64_t r0;
   int c0;
-  __device__ Place() {
+  __device__ Place(unsigned row_block, unsigned column_block) {
     constexpr int N = N_OF<S>, SIDE = 64 / N;
     const int lane = threadIdx.x & 63;
-    r0 = (int64_t)blockIdx.x * (N * N) + (lane / SIDE) * N;
-    c0 = blockIdx.y * 256 + (threadIdx.x >> 6) * 64 + (lane % SIDE) * N;
+    r0 = (int64_t)row_block * (N * N) + (lane / SIDE) * N;
+    c0 = (int)column_block * 256 + (int)(threadIdx.x >> 6) * 64 + (lane % SIDE) * N;
   }
 };
-template <typename S>
-dim3 grid_of(int64_t rows, int64_t columns) {
-  return dim3((unsigned)ceil_div(rows, (int64_t)N_OF<S> * N_OF<S>), (unsigned)ceil_div(columns, 256));
+template <typename S> int64_t row_blocks(int64_t rows) { return ceil_div(rows, (int64_t)N_OF<S> * N_OF<S>); }
+int64_t column_blocks(int64_t columns) { return ceil_div(columns, 256); }
+
+// Several jobs in one launch: workgroups end[j - 1] .. end[j] - 1 work on job j.  (A launch of its own each costs 2 to 4 us, as much as
+// the job itself takes with a few hundred rows.)
+template <typename J>
+struct Jobs {
+  J job[MAX_JOBS];
+  unsigned end[MAX_JOBS];
+  int n;
+};
+template <typename J>
+__device__ __forceinline__ int find_job(const Jobs<J>& p, unsigned* block) {
+  int j = 0;
+  while (j + 1 < p.n && blockIdx.x >= p.end[j]) ++j;
+  *block = blockIdx.x - (j ? p.end[j - 1] : 0u);
+  return j;
 }
 
 struct TransposeArgs {
-  const char* X;
-  int64_t R, k0, k_end;
-  int C;
-  Operand out, straight;
+  TransposeJob t;
+  unsigned rows;                             // row blocks
 };
 
 template <typename S>
-__global__ __launch_bounds__(256) void transpose_kernel(TransposeArgs p) {
+__global__ __launch_bounds__(256, 6) void transpose_kernel(Jobs<TransposeArgs> jobs) {
   constexpr int N = N_OF<S>;
-  const Place<S> at;
+  unsigned block;
+  const TransposeArgs& a = jobs.job[find_job(jobs, &block)];
+  const TransposeJob& p = a.t;
+  const Place<S> at(block % a.rows, block / a.rows);
   if (at.c0 >= p.C) return;
   u32x4 in[N], out[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     in[i] = u32x4{0, 0, 0, 0};
     const int64_t r = at.r0 + i;
-    if (r < p.R) {
-      in[i] = *(const u32x4*)(p.X + (r * p.C + at.c0) * sizeof(S));
-      if (p.straight.p) *chunk_of<S>(p.straight, r, at.c0) = in[i];
-    }
+    if (r < p.R) in[i] = *(const u32x4*)((const char*)p.X + (r * p.C + at.c0) * sizeof(S));
   }
+  if (p.straight.p)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at.r0 + i < p.R) *chunk_of<S>(p.straight, at.r0 + i, at.c0) = in[i];
   if (p.k0 + at.r0 >= p.k_end) return;
   transposed<S>(in, out);
 #pragma unroll
@@ -118,7 +134,7 @@ __device__ __forceinline__ u32x4 rounded(const float (&x)[N_OF<S>]) {
 template <typename S>
 __global__ __launch_bounds__(256) void branch_gradients_kernel(BranchArgs p) {
   constexpr int N = N_OF<S>;
-  const Place<S> at;
+  const Place<S> at(blockIdx.x, blockIdx.y);
   if (at.c0 >= p.F || at.r0 >= p.da_t.K) return;
   u32x4 a[N], b[N], h[N], out[N];
 #pragma unroll
@@ -177,21 +193,24 @@ __global__ __launch_bounds__(256) void silu_product_kernel(const f32x4* g, const
 }
 
 template <typename S>
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float* part, int parts, int64_t stride, int64_t n, S* out) {
+__global__ __launch_bounds__(256) void sum_parts_kernel(Jobs<SumJob> jobs) {
   constexpr int N = N_OF<S>;
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
-  if (i >= n) return;
+  unsigned block;
+  const SumJob& p = jobs.job[find_job(jobs, &block)];
+  const int64_t i = ((int64_t)block * 256 + threadIdx.x) * N;
+  if (i >= p.n) return;
   float x[N];
 #pragma unroll
-  for (int j = 0; j < N; j += 4) *(f32x4*)(x + j) = *(const f32x4*)(part + i + j);
-  for (int q = 1; q < parts; ++q)
+  for (int j = 0; j < N; j += 4) *(f32x4*)(x + j) = *(const f32x4*)(p.part + i + j);
+#pragma unroll 4
+  for (int q = 1; q < p.parts; ++q)
 #pragma unroll
     for (int j = 0; j < N; j += 4) {
-      const f32x4 y = *(const f32x4*)(part + q * stride + i + j);
+      const f32x4 y = *(const f32x4*)(p.part + q * p.stride + i + j);
 #pragma unroll
       for (int v = 0; v < 4; ++v) x[j + v] += y[v];
     }
-  *(u32x4*)(out + i) = rounded<S>(x);
+  *(u32x4*)((S*)p.out + i) = rounded<S>(x);
 }
 
 __global__ __launch_bounds__(256) void clear_kernel(u32x4* p, int64_t n) {
@@ -204,12 +223,21 @@ size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt) {
   return dt == MOEP_BF16 ? (size_t)ceil_div(rows, 256) * 256 * (size_t)K * 2 : (size_t)rows * (size_t)K * 4;
 }
 
-int launch_transpose(const void* X, int64_t R, int C, moep_dtype dt, const Operand& out, int64_t k0, int64_t k_end, const Operand* straight,
-                     hipStream_t s, const char* name) {
-  TransposeArgs p = {(const char*)X, R, k0, k_end, C, out, straight ? *straight : Operand{}};
-  Timed t(name, s);
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(transpose_kernel<uint16_t>, grid_of<uint16_t>(k_end - k0, C), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(transpose_kernel<float>, grid_of<float>(k_end - k0, C), dim3(256), 0, s, p);
+int launch_transposes(const TransposeJob* jobs, int n, moep_dtype dt, hipStream_t s) {
+  if (n < 1 || n > MAX_JOBS) return fail(MOEP_EINVAL, "transposes: %d jobs", n);
+  Jobs<TransposeArgs> p = {};
+  p.n = n;
+  int64_t blocks = 0;
+  for (int j = 0; j < n; ++j) {
+    const int64_t rows = dt == MOEP_BF16 ? row_blocks<uint16_t>(jobs[j].k_end - jobs[j].k0) : row_blocks<float>(jobs[j].k_end - jobs[j].k0);
+    p.job[j] = {jobs[j], (unsigned)rows};
+    blocks += rows * column_blocks(jobs[j].C);
+    if (blocks >= (int64_t)1 << 31) return fail(MOEP_EUNSUPPORTED, "transposes: too large");
+    p.end[j] = (unsigned)blocks;
+  }
+  Timed t("transpose", s);
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(transpose_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(transpose_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, p);
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
@@ -219,8 +247,8 @@ int launch_gradients_of_branches(const float* dh, int parts, const float* g, con
   BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, dab, da_t, db_t, h_t};
   if (!p.da_t.p) p.da_t.K = T;
   Timed t("branch_gradients", s);
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(branch_gradients_kernel<uint16_t>, grid_of<uint16_t>(p.da_t.K, F), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(branch_gradients_kernel<float>, grid_of<float>(p.da_t.K, F), dim3(256), 0, s, p);
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(branch_gradients_kernel<uint16_t>, dim3((unsigned)row_blocks<uint16_t>(p.da_t.K), (unsigned)column_blocks(F)), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(branch_gradients_kernel<float>, dim3((unsigned)row_blocks<float>(p.da_t.K), (unsigned)column_blocks(F)), dim3(256), 0, s, p);
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
@@ -232,11 +260,21 @@ int launch_silu_product(const float* g, const float* u, int64_t n, float* h, hip
   return MOEP_OK;
 }
 
-int launch_sum_parts(const float* part, int parts, int64_t stride, int64_t n, moep_dtype dt, void* out, hipStream_t s) {
+int launch_sums(const SumJob* jobs, int n, moep_dtype dt, hipStream_t s) {
+  if (n < 1) return MOEP_OK;
+  if (n > MAX_JOBS) return fail(MOEP_EINVAL, "sums: %d jobs", n);
+  Jobs<SumJob> p = {};
+  p.n = n;
+  int64_t blocks = 0;
+  for (int j = 0; j < n; ++j) {
+    p.job[j] = jobs[j];
+    blocks += ceil_div(jobs[j].n, 256 * (dt == MOEP_BF16 ? 8 : 4));
+    if (blocks >= (int64_t)1 << 31) return fail(MOEP_EUNSUPPORTED, "sums: too large");
+    p.end[j] = (unsigned)blocks;
+  }
   Timed t("sum_parts", s);
-  const unsigned blocks = (unsigned)ceil_div(n, 256 * (dt == MOEP_BF16 ? 8 : 4));
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, dim3(blocks), dim3(256), 0, s, part, parts, stride, n, (uint16_t*)out);
-  else hipLaunchKernelGGL(sum_parts_kernel<float>, dim3(blocks), dim3(256), 0, s, part, parts, stride, n, (float*)out);
+  if (dt == MOEP_BF16) hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(sum_parts_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, p);
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }

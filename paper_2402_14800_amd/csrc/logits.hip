@@ -24,12 +24,11 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned long long u64x2;
 
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr int NC = 16;                       // chunks of a tile per thread
-constexpr int CANDIDATES = 512;              // room for the elements that the search for the best sorts
-
 // Elements of a chunk: 4 fp32 or 8 bf16.
 template <typename S> struct Elements;
 template <> struct Elements<float> {
@@ -160,6 +159,21 @@ __device__ __forceinline__ void cut_ends(const Row<S>& row, int tile, int tid, u
   }
 }
 
+// A wavefront's values joined, the same in all lanes: over each 16 lanes, then the sixteens, from lane to lane in the registers (through LDS,
+// as an exchange of any lanes goes, six steps take a microsecond).
+template <typename T, typename F>
+__device__ __forceinline__ T over_wave(T x, T identity, F join) {
+  static_assert(sizeof(T) == 4, "");
+#define MOEP_FROM(ctrl, rows) \
+  x = join(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, identity), __builtin_bit_cast(int, x), ctrl, rows, 0xf, false)))
+  MOEP_FROM(0x111, 0xf); MOEP_FROM(0x112, 0xf); MOEP_FROM(0x114, 0xf); MOEP_FROM(0x118, 0xf);   // the lane 1, 2, 4, 8 before
+  MOEP_FROM(0x142, 0xa); MOEP_FROM(0x143, 0xc);                                                // lane 15 of the sixteen, 31 of the half before
+#undef MOEP_FROM
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ __forceinline__ float max_over_wave(float x) { return over_wave(x, NEG_INF, [](float a, float b) { return max_nan(a, b); }); }
+__device__ __forceinline__ float sum_over_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
+
 // A number that is the same in all lanes, moved to where it takes no register of theirs.
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
@@ -234,27 +248,27 @@ __device__ __forceinline__ void add_tile(u32x4 (&v)[NC], int chunks_left, Stats&
   a.w += w[0] + w[1];
 }
 
-// The workgroup's joint statistics, the same in every thread; `shared`: 3 floats per wavefront.  Joined in a fixed order.
+// The workgroup's joint statistics, the same in every thread, in two halves with a barrier between them: each wavefront's into `shared`
+// (3 floats a wavefront), then those of all, in a fixed order.
 template <int B, bool ENTROPY>
-__device__ __forceinline__ Stats join(Stats a, float c, float* shared) {
+__device__ __forceinline__ Stats join_wave(Stats a, float c, float* shared) {
   constexpr int WAVES = B / 64;
-  float m = a.m;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = max_nan(m, __shfl_xor(m, o));
-  a = moved<ENTROPY>(a, m, c);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    a.s += __shfl_xor(a.s, o);
-    if (ENTROPY) a.w += __shfl_xor(a.w, o);
-  }
-  if (WAVES == 1) return a;
-  if ((threadIdx.x & 63) == 0) {
+  a = moved<ENTROPY>(a, max_over_wave(a.m), c);
+  a.s = sum_over_wave(a.s);
+  if (ENTROPY) a.w = sum_over_wave(a.w);
+  if (WAVES > 1 && (threadIdx.x & 63) == 0) {
     const int wave = threadIdx.x >> 6;
     shared[wave] = a.m; shared[WAVES + wave] = a.s; shared[2 * WAVES + wave] = a.w;
   }
-  __syncthreads();
+  return a;
+}
+template <int B, bool ENTROPY>
+__device__ __forceinline__ Stats join_all(const Stats& a, float c, const float* shared) {
+  constexpr int WAVES = B / 64;
+  if (WAVES == 1) return a;
+  float m = shared[0];
 #pragma unroll
-  for (int q = 0; q < WAVES; ++q) m = max_nan(m, shared[q]);
+  for (int q = 1; q < WAVES; ++q) m = max_nan(m, shared[q]);
   Stats t = {m, 0.f, 0.f};
 #pragma unroll
   for (int q = 0; q < WAVES; ++q) {
@@ -281,10 +295,15 @@ struct LogprobArgs {
 
 template <int B>
 struct SearchSpace {
-  unsigned key[B];                           // of each thread's largest element
-  unsigned long long candidate[CANDIDATES];  // key << 32 | ~index: larger is better, and no two are alike
+  // Chunks with an element that reaches the threshold: each wavefront's in the order it met them, and where they begin in the row.
+  // (one wavefront gets less room, so that twenty of them fit a compute unit)
+  static constexpr int HITS = B == 64 ? 128 : B >= 1024 ? 48 : 512 / (B / 64), CANDIDATES = B == 64 ? 256 : 512;
+  u32x4 hit[B / 64 * HITS];
+  int hit_at[B / 64 * HITS];
+  unsigned threshold_of[2][B / 64];          // the wavefronts', of this tile and the one before
+  __attribute__((aligned(16))) unsigned long long candidate[CANDIDATES];   // key << 32 | ~index: larger is better, and no two are alike
   unsigned hist[256];
-  unsigned threshold;
+  unsigned threshold;                        // (of the exact search)
   int count, need;
 };
 
@@ -332,83 +351,131 @@ __device__ void select_exactly(const S* z, int V, int K, SearchSpace<B>* q) {
     const unsigned k = order_key(Elements<S>::load(z + i));
     if (k > prefix || (k == prefix && (unsigned)i <= index)) {
       const int at = atomicAdd(&q->count, 1);
-      if (at < CANDIDATES) q->candidate[at] = ((unsigned long long)k << 32) | (unsigned)~i;   // (K of them)
+      if (at < q->CANDIDATES) q->candidate[at] = ((unsigned long long)k << 32) | (unsigned)~i;   // (K of them)
     }
   }
   __syncthreads();
 }
 
-// The K best of a row.  Every thread knows the largest of the elements it has seen; at least K of those are no smaller than the K-th
-// largest of them, which is therefore a threshold that the K best reach, and few others do (256 threads, K = 64: about 74 elements of a
-// tile).  After every tile the threshold is found anew and the tile's elements that reach it are collected, in any order, while they are in
-// registers; what an earlier, lower threshold let in does no harm.  At the end the candidates are sorted by counting, each against all; no
-// two compare equal, so the result has one order.
+// The K best of a row.  Every thread knows the largest of the elements it has seen; if of each of W wavefronts K / W threads' reach a
+// threshold, K elements do, the K best among them, and few others (256 threads, K = 64: about 90 elements of a tile).  After every tile
+// the threshold is found anew, each wavefront's by itself and the least of them, and the tile's chunks that hold an element which reaches it
+// are set aside in LDS while they are in registers; what an earlier, lower threshold let in does no harm.  At the end every lane takes such a
+// chunk, and the elements that reach the last threshold are sorted by counting, each against all; no two compare equal, so the result has
+// one order.
 
-// The largest key that at least K of the threads' largest elements reach (bf16: to 16 bits, which is exact; more threads than 256 in fours,
-// since their number is what the search costs); 0 if they are fewer.
-template <typename S, int B>
-__device__ __forceinline__ float find_threshold(float own, bool seen, int K, bool first, SearchSpace<B>* q) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  q->key[tid] = seen ? order_key(own) : 0u;
-  __syncthreads();
-  if (tid < 64) {
-    constexpr int GROUPS = B >= 256 ? 4 : B / 64, EACH = B / (64 * GROUPS);
-    unsigned k[GROUPS];
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      k[g] = 0;
-#pragma unroll
-      for (int e = 0; e < EACH; ++e) k[g] = max(k[g], q->key[(e * GROUPS + g) * 64 + lane]);
-    }
-    unsigned found = 0;
-#pragma unroll 1
-    for (int b = 31; b >= (sizeof(S) == 2 ? 16 : 0); --b) {
-      const unsigned at = found | (1u << b);
-      int n = 0;
-#pragma unroll
-      for (int g = 0; g < GROUPS; ++g) n += __popcll(__ballot(k[g] >= at));
-      if (n >= K) found = at;
-    }
-    if (lane == 0) {
-      q->threshold = found;
-      if (first) q->count = 0;
+// A key that at least `need` lanes' reach, and hardly more: `need` plus an eighth.  By bits from two octaves below the largest (most often
+// there), else from all of them.  0 if there are not so many.
+__device__ __forceinline__ unsigned reached_by(unsigned key, int need, int lowest_bit) {
+  const unsigned top = over_wave(key, 0u, [](unsigned a, unsigned b) { return max(a, b); });
+  if (need == 1) return top;
+  constexpr unsigned TWO_OCTAVES = 1u << 24;
+  unsigned found = top > TWO_OCTAVES ? (top - TWO_OCTAVES) & ~0xffffu : 0u;
+  int bit = 23;
+  if (__popcll(__ballot(key >= found)) < need) { found = 0; bit = 31; }
+  for (; bit >= lowest_bit; --bit) {
+    const unsigned at = found + (1u << bit);
+    const int n = __popcll(__ballot(key >= at));
+    if (n >= need) {
+      found = at;
+      if (n <= need + (need >> 3)) break;
     }
   }
-  __syncthreads();
-  const unsigned threshold = q->threshold;
-  return threshold <= 0x007fffffu ? NEG_INF : key_value(threshold);     // (too few: everything)
+  return found;
 }
 
-// The elements of a tile that reach `least`.
+// The threshold in two halves with a barrier between them, like the statistics.
 template <typename S, int B>
-__device__ __forceinline__ void collect(const Row<S>& row, const u32x4 (&v)[NC], int tile, int tid, float least, SearchSpace<B>* q) {
-  constexpr int N = Elements<S>::N;
+__device__ __forceinline__ unsigned threshold_of_wave(float own, bool seen, int chunks, int K, int turn, SearchSpace<B>* q) {
+  constexpr int WAVES = B / 64;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // the wavefronts all of whose threads have seen something; one where none has
+  const int full = max(1, min(WAVES, chunks / 64));
+  unsigned found = ~0u;
+  if (wave < full) found = reached_by(seen ? order_key(own) : 0u, (K + full - 1) / full, sizeof(S) == 2 ? 16 : 0);
+  if (WAVES > 1 && (threadIdx.x & 63) == 0) q->threshold_of[turn][wave] = found;
+  return found;
+}
+template <int B>
+__device__ __forceinline__ float threshold_of_all(unsigned found, int turn, const SearchSpace<B>* q) {
+  if (B > 64)
+#pragma unroll
+    for (int w = 0; w < B / 64; ++w) found = min(found, q->threshold_of[turn][w]);
+  found = (unsigned)__builtin_amdgcn_readfirstlane((int)found);
+  return found <= 0x007fffffu ? NEG_INF : key_value(found);  // (too few: everything)
+}
+
+// Sets aside the chunks of a tile with an element that reaches `least`; `hits`: the wavefront's, before and after (beyond HITS: not kept).
+template <typename S, int B>
+__device__ __forceinline__ int set_aside(const Row<S>& row, const u32x4 (&v)[NC], int tile, int tid, float least, int hits, SearchSpace<B>* q) {
+  constexpr int N = Elements<S>::N, HITS = SearchSpace<B>::HITS;
   const int c0 = tile * (B * NC);
+  const int first = __builtin_amdgcn_readfirstlane(tid >> 6) * HITS;
+  auto walk = [&](auto some) {
 #pragma unroll
-  for (int n = 0; n < NC; ++n)
-    if (c0 + n * B < row.chunks) {                           // (the same for all threads)
-      bool some;
-      if (sizeof(S) == 2 && least > 0.f) {                   // (the same for all threads; bits of positive numbers are in their order)
-        const s16x2 top = top_halves(v[n]);
-        some = max(top[0], top[1]) >= (short)(__float_as_uint(least) >> 16);
-      } else {
-        float m = Elements<S>::get(v[n], 0);
-#pragma unroll
-        for (int j = 1; j < N; ++j) m = fmaxf(m, Elements<S>::get(v[n], j));
-        some = m >= least;
-      }
-      if (some) {
-        const int i0 = (c0 + n * B + tid) * N - row.lead;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float z = Elements<S>::get(v[n], j);
-          if (z >= least && i0 + j >= 0 && i0 + j < row.V) {
-            const int at = atomicAdd(&q->count, 1);
-            if (at < CANDIDATES) q->candidate[at] = ((unsigned long long)order_key(z) << 32) | (unsigned)~(i0 + j);
-          }
+    for (int n = 0; n < NC; ++n)
+      if (c0 + n * B < row.chunks) {                         // (the same for all threads)
+        const bool mine = some(v[n]);
+        const unsigned long long mask = __ballot(mine);
+        const int at = hits + __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+        if (mine && at < HITS) {
+          q->hit[first + at] = v[n];
+          q->hit_at[first + at] = (c0 + n * B + tid) * N - row.lead;
         }
+        hits += __popcll(mask);
       }
+  };
+  if (sizeof(S) == 2 && least > 0.f) {                       // (bits of numbers that are not negative are in their order)
+    const short bits = (short)(__float_as_uint(least) >> 16);
+    walk([&](const u32x4& x) {
+      const s16x2 top = top_halves(x);
+      return max(top[0], top[1]) >= bits;
+    });
+  } else {
+    walk([&](const u32x4& x) {
+      float m = Elements<S>::get(x, 0);
+#pragma unroll
+      for (int j = 1; j < N; ++j) m = fmaxf(m, Elements<S>::get(x, j));
+      return m >= least;
+    });
+  }
+  return hits;
+}
+
+// The elements that reach `least` of the chunks that the wavefront has set aside: into the workgroup's list.
+template <typename S, int B>
+__device__ __forceinline__ void expand(int V, int hits, float least, SearchSpace<B>* q) {
+  constexpr int N = Elements<S>::N, HITS = SearchSpace<B>::HITS;
+  const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * HITS;
+  if (hits > HITS) {                                         // not all were kept: the exact search
+    if (lane == 0) atomicAdd(&q->count, q->CANDIDATES + 1);
+    return;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (int h0 = 0; h0 < hits; h0 += 64) {
+    const bool there = h0 + lane < hits;
+    const u32x4 x = there ? q->hit[first + h0 + lane] : neutral<S>();
+    const int i0 = there ? q->hit_at[first + h0 + lane] : V;
+    unsigned long long mask[N];
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      mask[j] = __ballot(Elements<S>::get(x, j) >= least && i0 + j >= 0 && i0 + j < V);
+      n += __popcll(mask[j]);
     }
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&q->count, n);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if ((mask[j] >> lane) & 1) {
+        const int k = at + __builtin_amdgcn_mbcnt_hi((unsigned)(mask[j] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask[j], 0u));
+        if (k < q->CANDIDATES) q->candidate[k] = ((unsigned long long)order_key(Elements<S>::get(x, j)) << 32) | (unsigned)~(i0 + j);
+      }
+      at += __popcll(mask[j]);
+    }
+  }
 }
 
 template <typename S, int B>
@@ -421,16 +488,25 @@ __device__ __forceinline__ void write_best(const S* row, const LogprobArgs& p, c
     for (int j = tid; j < p.K; j += B) { out[j] = all.s; ids[j] = j; }
     return;
   }
-  if (q->count > CANDIDATES) {                               // (the same for all threads)
+  if (q->count > q->CANDIDATES) {                               // (the same for all threads)
     __syncthreads();
     select_exactly<S, B>(row, p.V, p.K, q);
   }
   const int n = q->count;
-  for (int i = tid; i < n; i += B) {
-    const unsigned long long mine = q->candidate[i];
+  // A candidate's rank: how many are larger.  Where there are few of them, several threads share the counting.
+  const int share = 4 * n <= B ? 2 : 2 * n <= B ? 1 : 0, part = tid & ((1 << share) - 1);
+  for (int i0 = 0; i0 < n; i0 += B >> share) {
+    const int i = i0 + (tid >> share);
+    const unsigned long long mine = i < n ? q->candidate[i] : ~0ull;
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += q->candidate[j] > mine;
-    if (rank < p.K) {
+#pragma unroll 4
+    for (int j = 2 * part; j < n; j += 2 << share) {
+      const u64x2 x = *(const u64x2*)(q->candidate + j);
+      rank += (x[0] > mine) + (j + 1 < n && x[1] > mine);
+    }
+    if (share > 0) rank += __shfl_xor(rank, 1);
+    if (share > 1) rank += __shfl_xor(rank, 2);
+    if (i < n && part == 0 && rank < p.K) {
       const float z = key_value((unsigned)(mine >> 32));
       ids[rank] = (int32_t)~(unsigned)mine;
       out[rank] = all.m == NEG_INF ? NEG_INF : (z - all.m) - log_s;
@@ -448,28 +524,40 @@ __global__ __launch_bounds__(B) void token_logprobs_kernel(LogprobArgs p) {
   const int64_t y = p.tokens[t];
   u32x4 v[NC];
   Stats own = {NEG_INF, 0.f, 0.f};
-  for (int tile = 0; tile * (B * NC) < row.chunks; ++tile) {
+  if (tid == 0) search.count = 0;
+  int hits = 0;
+  float least = NEG_INF, zy = 0.f;
+  const int tiles = (row.chunks + B * NC - 1) / (B * NC);
+  for (int tile = 0; tile < tiles; ++tile) {
     tid = thread_again(tid);
     request_tile<S, B>(row, tile, tid, v);
     cut_ends<S, B>(row, tile, tid, v);
     add_tile<S, B, true>(v, row.chunks - tile * (B * NC), own, LOG2E);
+    // (after the tile's own loads have been waited for one by one: a load that only some lanes make ends that)
+    if (tile + 1 == tiles && tid == 0 && y >= 0 && y < p.V) zy = Elements<S>::load(row.at + y);
+    unsigned found = 0;
+    if (p.K > 0) found = threshold_of_wave<S, B>(own.m, tid < row.chunks, row.chunks, p.K, tile & 1, &search);
+    if (tile + 1 == tiles) own = join_wave<B, true>(own, LOG2E, shared);
+    else if (p.K == 0) continue;
+    __syncthreads();
     if (p.K > 0) {
-      const float least = find_threshold<S, B>(own.m, tid < row.chunks, p.K, tile == 0, &search);
+      least = threshold_of_all<B>(found, tile & 1, &search);
       use_again(v);
-      collect<S, B>(row, v, tile, tid, least, &search);
+      hits = set_aside<S, B>(row, v, tile, tid, least, hits, &search);
     }
   }
-  const Stats all = join<B, true>(own, LOG2E, shared);
+  const Stats all = join_all<B, true>(own, LOG2E, shared);
   if (tid == 0) {
     const float log_s = logf(all.s);
     float lp = 0.f;                                          // no token given
     if (y >= p.V) lp = __builtin_nanf("");
-    else if (y >= 0) lp = all.m == NEG_INF ? NEG_INF : (Elements<S>::load(row.at + y) - all.m) - log_s;
+    else if (y >= 0) lp = all.m == NEG_INF ? NEG_INF : (zy - all.m) - log_s;
     p.logprob[t] = lp;
     p.entropy[t] = all.m == NEG_INF ? 0.f : max_nan(log_s - all.w / all.s, 0.f);
   }
   if (p.K > 0) {
-    if (B == 64) __syncthreads();                            // (more wavefronts met in join)
+    expand<S, B>(p.V, hits, least, &search);
+    __syncthreads();
     write_best<S, B>(row.at, p, all, t, &search);
   }
 }
@@ -516,14 +604,12 @@ __device__ __forceinline__ bool weigh(const DistillArgs& p, const Alternatives& 
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     if (a.id[h] >= 0) m = max_nan(m, a.x[h]);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = max_nan(m, __shfl_xor(m, o));
+  m = max_over_wave(m);
   const float r = reference(m);                              // (no alternative is there: everything below is 0)
   float s = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) { q[h] = a.id[h] >= 0 ? exp2_fast((a.x[h] - r) * c) : 0.f; s += q[h]; }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  s = sum_over_wave(s);
   const float log_s = logf(s);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -633,13 +719,15 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
       add_tile<S, B, false>(v, row.chunks - i * (B * NC), all, c);
     }
     keep_logits();
-    all = join<B, false>(all, c, shared);
+    all = join_wave<B, false>(all, c, shared);
+    __syncthreads();                                         // (`present` is there too)
+    all = join_all<B, false>(all, c, shared);
     m = uniform(all.m); log_s = uniform(logf(all.s)); inv_s = uniform(1.f / all.s);
   } else {
     m = uniform(p.stats[2 * t]); log_s = uniform(p.stats[2 * t + 1]);
     keep_logits();
+    __syncthreads();
   }
-  if (MODE == GRADIENT || B == 64) __syncthreads();          // `present` is there (more wavefronts met in join)
   // No alternative, or no logit above -inf: nothing to learn from.
   const bool nothing = !__builtin_amdgcn_readfirstlane(present) || m == NEG_INF;
   if (MODE != GRADIENT && tid < 64) {
@@ -651,8 +739,7 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
         const float q = teacher.q[j];
         if (teacher.id[j] >= 0 && !(q == 0.f)) x += q * (teacher.log_q[j] - ((teacher.z[j] - m) / p.tau - log_s));
       }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    x = sum_over_wave(x);
     if (tid == 0) {
       p.loss[t] = p.tau * p.tau * x;
       p.stats[2 * t] = m;
@@ -706,15 +793,17 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
 int threads_to_hold(int64_t T, int64_t chunks) {
   if (chunks > 1024 * NC) return 0;
   if (T <= 512 && chunks > 256) return 1024;
-  for (int b : {64, 128, 256, 512})
-    if (chunks <= b * NC) return b;
-  return 1024;
+  if (chunks <= 64 * NC) return 64;
+  if (chunks <= 128 * 12) return 128;                        // (of 16 that there is room for)
+  if (chunks <= 256 * (T < 2048 ? NC : 14)) return 256;
+  return chunks <= 512 * NC ? 512 : 1024;
 }
-// Threads per row of log probabilities, which need not be held: one wavefront where that holds the row, else 256, of few rows more.
+// Threads per row of log probabilities, which need not be held: one wavefront where that holds the row, else 256, of few rows more (and at
+// most two tiles then).
 int threads_to_read(int64_t T, int64_t chunks) {
   if (chunks <= 64 * NC && T > 2048) return 64;
   for (int b : {256, 512})
-    if (T * b >= 150000 || chunks <= b) return b;
+    if ((T * b >= 150000 && (T >= 1024 || chunks <= 2 * b * NC)) || chunks <= b) return b;
   return 1024;
 }
 // Chunks of a row at most: its elements from the 16-byte boundary before it on, which is as far for every row where `ld` is whole chunks.
@@ -755,7 +844,7 @@ int launch_distill(const DistillArgs& p, int64_t T, moep_dtype dt, hipStream_t s
     else hipLaunchKernelGGL((distill_topk_kernel<float, B, MODE, HELD>), dim3((unsigned)T), dim3(B), 0, s, p);
   };
   if (threads) with_threads(threads, [&](auto b) { with(b, std::true_type{}); });
-  else with(std::integral_constant<int, 512>{}, std::false_type{});
+  else with(std::integral_constant<int, 1024>{}, std::false_type{});
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
@@ -785,7 +874,7 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
   LogprobArgs p = {logits, ld, T, (int)V, tokens, K, logprob, entropy, top_logprob, top_ids};
   hipStream_t s = (hipStream_t)hip_stream;
   int threads = threads_to_read(T, most_chunks(logits, ld, V, dt));
-  while (threads < 256 && 2 * K > threads) threads *= 2;     // (a threshold from few more than K threads lets too many through)
+  if (threads == 64 && K > 32) threads = 128;                // (a threshold from few more than K threads lets too many through)
   Timed timed("token_logprobs", s);
   with_threads(threads, [&](auto b) {
     constexpr int B = decltype(b)::value;
