@@ -511,6 +511,7 @@ int expert_ffn_forward(const void* x, const void* W1, const void* W3, const void
 // The backward call's workspace.  `t_parts` ranges along the tokens for dW2, half as many (where even) for dW1 and dW3, which have
 // twice the tiles; K of the transposed operands is T padded to whole ranges.
 struct FfnBackwardPlan {
+  bool together;                                  // the last three products in one launch (tile_plan.h)
   int dh_parts, dx_parts, t_parts, t_parts13;
   int64_t Tp, rows13;                             // rows13: rows of da^T | db^T as one operand
   size_t dy, w2t, dh, dab, w13t, x_t, dy_t, dadb_t, h_t, dx_part, w13_part, w2_part, total;
@@ -520,6 +521,12 @@ static int plan_ffn_backward(int64_t T, int H, int F, moep_dtype dt, FfnBackward
   p->dx_parts = ranges_of(T, H, 2 * (int64_t)F, dt, false);
   p->t_parts = ranges_of(H, F, T, dt, true);
   p->t_parts13 = p->t_parts % 2 ? p->t_parts : p->t_parts / 2;
+  const BackwardCut cut = cut_backward(T, H, F);
+  p->together = dt == MOEP_BF16 && cut.together;
+  if (p->together) {
+    p->dx_parts = (int)cut.dx_ranges;
+    p->t_parts = p->t_parts13 = (int)cut.t_ranges;
+  }
   const int64_t unit = (dt == MOEP_BF16 ? 64 : p->t_parts > 1 ? 32 : 4) * (int64_t)p->t_parts;
   p->Tp = ceil_div(T, unit) * unit;
   if (p->Tp >= (int64_t)1 << 31) return fail(MOEP_EUNSUPPORTED, "expert_ffn_backward: T=%lld is too large", (long long)T);
@@ -608,6 +615,27 @@ int expert_ffn_backward(const void* dy, const void* x, const void* W1, const voi
                                             weights ? db_t : none, weights ? h_t : none, s)) return st;
   SumJob sums[MAX_JOBS];
   int n_sums = 0;
+  if (p.together) {
+    PackedProduct q[SEVERAL_MAX];
+    int n = 0;
+    auto product = [&](const Operand& A, const Operand& B, int ranges, size_t part, void* C) {
+      PackedProduct& g = q[n++];
+      g.A = A.p; g.B = B.p; g.M = A.rows; g.N = (int)B.rows; g.K = (int)A.K; g.ranges = ranges;
+      g.C = ranges > 1 ? at + part : C;
+      if (ranges > 1) {
+        SumJob& sum = sums[n_sums++];
+        sum.part = (const float*)g.C; sum.parts = ranges; sum.stride = sum.n = g.M * g.N; sum.out = C;
+      }
+    };
+    if (dx) product(dab, w13t, p.dx_parts, p.dx_part, dx);
+    if (weights) {
+      product(da_t, x_t, p.t_parts, p.w13_part, dW1);
+      product(db_t, x_t, p.t_parts, p.w13_part + (size_t)p.t_parts * F * H * 4, dW3);
+      product(dy_t, h_t, p.t_parts, p.w2_part, dW2);
+    }
+    if (int st = launch_gemm_bf16_several(q, n, s, "ffn_dx_dw")) return st;
+    return launch_sums(sums, n_sums, dt, s);
+  }
   if (dx) {
     const Product q = {dab.p, w13t.p, false, T, H, 2 * F, p.dx_parts};
     if (int st = multiply(q, dt, dx, (float*)(at + p.dx_part), sums, &n_sums, s, "ffn_dx")) return st;

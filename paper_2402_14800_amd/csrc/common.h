@@ -83,8 +83,10 @@ enum GemmEpilogue {
   EPI_ROWSCALE_F32 = 2, // C[m,n] = row_scale[m] * acc        (C in fp32)
   // the bf16 GEMMs of an expert's training step
   EPI_SWIGLU_KEEP = 3,  // EPI_SWIGLU, and both branches before the activation in fp32
-  EPI_STORE_F32 = 4     // C[m,n] = acc (C in fp32), one of `experts` sums over as many ranges of K
+  EPI_STORE_F32 = 4,    // C[m,n] = acc (C in fp32), one of `experts` sums over as many ranges of K
+  EPI_SEVERAL = 5       // several GEMMs in one launch, each with C in bf16, or in fp32 over ranges of its K
 };
+constexpr int SEVERAL_MAX = 4;
 constexpr bool gemm_pairs(int epilogue) { return epilogue == EPI_SWIGLU || epilogue == EPI_SWIGLU_KEEP; }
 
 struct GemmArgs {
@@ -168,6 +170,15 @@ struct PackedGemmArgs {
 // The epilogues of the training step (dense): EPI_SWIGLU_KEEP on row-major weights; EPI_STORE_F32, where `experts` ranges of K
 // of ONE GEMM (K and the operands are the whole ones) give as many sums of products, c_expert_bytes apart.
 int launch_gemm_bf16_train(const PackedGemmArgs& g, hipStream_t s, const char* name);
+// C [M,N] = A B^T of packed operands, bf16, or (ranges > 1) `ranges` fp32 matrices of as many ranges of K, one after the other.
+struct PackedProduct {
+  const void* A = nullptr;
+  const void* B = nullptr;
+  void* C = nullptr;
+  int64_t M = 0;
+  int N = 0, K = 0, ranges = 1;
+};
+int launch_gemm_bf16_several(const PackedProduct* q, int n, hipStream_t s, const char* name);   // n <= SEVERAL_MAX
 int allow_train_gemms();           // (by gemm_device_ready)
 size_t packed_a_bytes(int64_t rows, int K);
 size_t packed_b_bytes(int N, int K, bool gate_up_pair);

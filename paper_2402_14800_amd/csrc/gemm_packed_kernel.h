@@ -92,6 +92,17 @@ __host__ __device__ constexpr int perm32(int p) {
 }
 
 // ---- GEMM --------------------------------------------------------------------------------------
+// EPI_SEVERAL: one of the GEMMs of a launch.  Its K is cut into `ranges` ranges of nsl slices each (wide_nsl in all); range r goes to
+// C + r c_range_bytes.
+struct KProblem {
+  const char* A; const char* B;
+  void* C;
+  int64_t M, ldc, c_range_bytes;
+  int N, nsl, wide_nsl, m_tiles, n_tiles;
+  uint32_t end;           // tiles of the GEMMs up to this one
+  bool f32;               // C in fp32
+};
+
 struct KArgs {
   const char* A;          // packed, tile-major
   const char* B;          // packed weight blocks; BROW: the weights as the caller stores them, row-major [N, K]
@@ -117,6 +128,8 @@ struct KArgs {
   uint16_t* direct_out;
   const uint32_t* tile_order;   // grouped mode: a header, then entry bid = (M tile << 12) | N tile
   int wide_nsl;                 // EPI_STORE_F32: slices of the operands' whole K, of which expert e walks nsl
+  KProblem several[SEVERAL_MAX];   // EPI_SEVERAL, with the most slices to a tile first
+  int problems;
 };
 
 // Round counters of the persistent workgroups, one per XCD (64 bytes apart); see round_sync in the kernel.
@@ -146,13 +159,15 @@ __device__ __forceinline__ void gemm_body() {
   const int wave = tid >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wm = wave_u >> 1, wn = wave_u & 1;
-  const int nsl = p.nsl;
-  const int wide_nsl = SPLIT ? p.wide_nsl : nsl;
+  constexpr bool SEVERAL = EPI == EPI_SEVERAL;     // tiles of several GEMMs: a "GEMM of a batch" e is a problem (e & 3) and a range of its K
+  static_assert(!SEVERAL || (!GROUPED && !BROW), "packed operands only");
+  const int nsl_of_all = SEVERAL ? 0 : p.nsl;
+  const int wide_nsl = SPLIT ? p.wide_nsl : nsl_of_all;
   // Grouped launches are sized for the largest possible tile map; the order says how many tiles there are: full-width ones first,
   // half-width ones after them.
   const uint32_t m_tiles = (uint32_t)p.m_tiles, n_tiles = (uint32_t)p.n_tiles;
   const uint32_t per_expert = m_tiles * n_tiles;
-  const uint32_t nblk = GROUPED ? p.tile_order[NG == 8 ? TILE_ORDER_FULL : TILE_ORDER_HALF] : per_expert * (uint32_t)p.experts;
+  const uint32_t nblk = GROUPED ? p.tile_order[NG == 8 ? TILE_ORDER_FULL : TILE_ORDER_HALF] : SEVERAL ? p.several[p.problems - 1].end : per_expert * (uint32_t)p.experts;
   const uint32_t order_at = TILE_ORDER_HEADER + (GROUPED && NG == 4 ? p.tile_order[TILE_ORDER_FULL] : 0u);
   const uint32_t G = gridDim.x;
 
@@ -164,8 +179,20 @@ __device__ __forceinline__ void gemm_body() {
   const int pitch = wide_nsl * 64;
   const int brow_group = NG == 8 ? 32 * wave_u : 32 * (wave_u >> 1);
   const int brow_uni = NG == 8 ? 0 : 4 * (wave_u & 1) * pitch;
+  auto a_tile = [&](int tm_, int e_) -> const char* {
+    if (SEVERAL) {
+      const auto& q = p.several[e_ & 3];
+      return q.A + ((size_t)tm_ * q.wide_nsl + (size_t)(e_ >> 2) * q.nsl) * SLICE + wave_u * (MG * 512);
+    }
+    return p.A + (int64_t)e_ * p.a_expert_bytes + ((size_t)tm_ * wide_nsl) * SLICE + wave_u * (MG * 512);
+  };
   auto b_tile = [&](int tm_, int tn_, int e_, int unit) {
     const char* b;
+    if (SEVERAL) {
+      const auto& q = p.several[e_ & 3];
+      b = q.B + ((size_t)(NG == 8 ? tn_ : tn_ >> 1) * q.wide_nsl + (size_t)(e_ >> 2) * q.nsl) * SLICE;
+      return b + (NG == 8 ? wave_u * 4096 : (tn_ & 1) * 8192 + wave_u * 2048);
+    }
     if (BROW) {
       // a unit: 16 NG rows of either branch, or half of the tile's 32 NG; a wavefront brings 4 NG of them
       const int row = PAIR ? tn_ * (16 * NG) : tn_ * (32 * NG) + unit * (16 * NG);
@@ -192,6 +219,24 @@ __device__ __forceinline__ void gemm_body() {
       e = 0;
       tm = (int)(v >> 12);
       tn = (int)(v & 4095u);
+    } else if (SEVERAL) {
+      // Every XCD gets a contiguous run of each GEMM's tiles, so that they share operand panels in its L2, the GEMMs' longest tiles first.
+      // (Tiles that are left over go to the XCDs in turn, on from where those of the GEMM before ended: XCD x has as many tiles as there
+      // are ids x, x + 8, ...)  One flat order over all XCDs: the launch of 777 rows, H 1024, F 3584 took 47 us for SEVERAL_US.
+      int pi = 0;
+      uint32_t start = 0, at = j, turn = xcd, tiles = p.several[0].end;
+      while (at >= (tiles >> 3) + (turn < (tiles & 7) ? 1u : 0u) && pi + 1 < p.problems) {
+        at -= (tiles >> 3) + (turn < (tiles & 7) ? 1u : 0u);
+        start = p.several[pi].end;
+        turn = (xcd - start) & 7u;
+        tiles = p.several[++pi].end - start;
+      }
+      const uint32_t in_problem = turn * (tiles >> 3) + min(turn, tiles & 7u) + at, m = (uint32_t)p.several[pi].m_tiles;
+      const uint32_t of_range = m * (uint32_t)p.several[pi].n_tiles;
+      const uint32_t range = in_problem / of_range, rest = in_problem - range * of_range;
+      e = pi | (int)(range << 2);
+      tn = (int)(rest / m);
+      tm = (int)(rest % m);
     } else {
       uint32_t bid;
       if ((per_expert & 7) == 0 && nblk > G) {
@@ -226,7 +271,8 @@ __device__ __forceinline__ void gemm_body() {
   if (L_ld >= nblk) return;
   int tm_ld, tn_ld, e_ld;
   decode(L_ld, tm_ld, tn_ld, e_ld);
-  const char* a_ld = p.A + (int64_t)e_ld * p.a_expert_bytes + ((size_t)tm_ld * wide_nsl) * SLICE + wave_u * (MG * 512);
+  const char* a_ld = a_tile(tm_ld, e_ld);
+  int nsl = SEVERAL ? p.several[e_ld & 3].nsl : nsl_of_all;   // of the loader's tile
   const char* b_ld = b_tile(tm_ld, tn_ld, e_ld, 0);
   // BROW: from the tile's first unit to its second
   const int64_t b1_branch = p.B1 - p.B;
@@ -286,7 +332,7 @@ __device__ __forceinline__ void gemm_body() {
   // thousand cycles apart); a workgroup that ran into the bound goes on alone and polls no more in this launch.  Only the
   // timing depends on any of this, never a result.
   const uint32_t rounds = (nblk + G - 1) / G;
-  const bool sync_on = nblk > G && (G & 7) == 0 && (G >> 3) < 65536u;
+  const bool sync_on = !SEVERAL && nblk > G && (G & 7) == 0 && (G >> 3) < 65536u;
   bool poll_ok = true;
   uint32_t switches = 0;
   auto round_sync = [&](bool wait) {
@@ -328,7 +374,8 @@ __device__ __forceinline__ void gemm_body() {
     }                                                                                           \
     if (L_ld < nblk) {                                                                          \
       decode(L_ld, tm_ld, tn_ld, e_ld);                                                         \
-      a_ld = p.A + (int64_t)e_ld * p.a_expert_bytes + ((size_t)tm_ld * wide_nsl) * SLICE + wave_u * (MG * 512); \
+      a_ld = a_tile(tm_ld, e_ld);                                                               \
+      if (SEVERAL) nsl = p.several[e_ld & 3].nsl;                                               \
       b_ld = b_tile(tm_ld, tn_ld, e_ld, 0);                                                     \
       if (BROW && !PAIR) b1_rows = (int)(b_tile(tm_ld, tn_ld, e_ld, 1) - b_ld);      \
     } else {                                                                                    \
@@ -481,8 +528,8 @@ __device__ __forceinline__ void gemm_body() {
     MOEP_ZERO_ACC()
     // The loader is NS - 1 slices ahead and changes tile between two runs of steps, never inside one.  K / 32
     // and NS - 1 are even, so every run is a whole number of step pairs.
-    for (int left = nsl; left > 0;) {
-      const int run = min(left, nsl - s_ld);
+    for (int left = SEVERAL ? p.several[e_mm & 3].nsl : nsl; left > 0;) {
+      const int run = SEVERAL && !ld_ok ? left : min(left, nsl - s_ld);
 #pragma unroll 1
       for (int s_mm = 0; s_mm < run; s_mm += 2) {
         MOEP_STEP(0, false)
@@ -501,12 +548,14 @@ __device__ __forceinline__ void gemm_body() {
     int lane_e;
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane_e));
     const int q8 = 8 * (lane_e >> 4);
-    int64_t row0 = (int64_t)tm * 256, row_end = p.M;
+    const auto& q_mm = p.several[SEVERAL ? e_mm & 3 : 0];
+    int64_t row0 = (int64_t)tm * 256, row_end = SEVERAL ? q_mm.M : p.M;
     if (GROUPED) {
       row0 = p.tile_row0[tm];
       row_end = p.seg_end[p.tile_expert[tm]];
     }
-    char* const c_base = (char*)p.C + (GROUPED ? (int64_t)0 : (int64_t)e_mm * p.c_expert_bytes);
+    char* const c_base = SEVERAL ? (char*)q_mm.C + (int64_t)(e_mm >> 2) * q_mm.c_range_bytes
+                                 : (char*)p.C + (GROUPED ? (int64_t)0 : (int64_t)e_mm * p.c_expert_bytes);
     // EPI_ROWSCALE_F32: scales and destinations of the wavefront's rows, 64 to a register, all fetched before the first is used
     // (row group by row group they were 16 round trips to memory, one after the other: E 16, H 2048, F 5632, top-4, 1001 tokens, this
     // launch 151 -> 147 us; Mixtral shape, 32768 tokens, the forward 13190 -> 13110)
@@ -573,20 +622,24 @@ __device__ __forceinline__ void gemm_body() {
 #pragma unroll
         for (int P = 0; P < NG / 2; ++P) {
           const int n = tn * (NG * 32) + wn * (NG * 16) + 32 * P + q8;
-          if (n >= p.N) continue;
-          if (EPI == EPI_STORE || (EPI == EPI_ROWSCALE_F32 && dest >= 0)) {
+          if (n >= (SEVERAL ? q_mm.N : p.N)) continue;
+          // (two ways to store: the tiles in vector registers from here on, as above)
+          f32x4 t[2] = {acc[i][2 * P], acc[i][2 * P + 1]};
+          if constexpr (SEVERAL) asm volatile("" : "+v"(t[0]), "+v"(t[1]));
+#define MOEP_OUT(x) (SEVERAL ? t[x] : acc[i][2 * P + (x)])
+          if (EPI == EPI_STORE || (SEVERAL && !q_mm.f32) || (EPI == EPI_ROWSCALE_F32 && dest >= 0)) {
             bf16x2 o[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const f32x2 h = {acc[i][2 * P + (c >> 1)][2 * (c & 1)], acc[i][2 * P + (c >> 1)][2 * (c & 1) + 1]};
+              const f32x2 h = {MOEP_OUT(c >> 1)[2 * (c & 1)], MOEP_OUT(c >> 1)[2 * (c & 1) + 1]};
               o[c] = __builtin_convertvector(h, bf16x2);
             }
-            uint16_t* const row = EPI == EPI_STORE ? (uint16_t*)c_base + r * p.ldc : p.direct_out + (int64_t)dest * p.ldc;
+            uint16_t* const row = EPI == EPI_STORE || SEVERAL ? (uint16_t*)c_base + r * (SEVERAL ? q_mm.ldc : p.ldc) : p.direct_out + (int64_t)dest * p.ldc;
             *(u32x4*)(row + n) = __builtin_bit_cast(u32x4, o);
-          } else {                                               // EPI_ROWSCALE_F32, EPI_STORE_F32
-            float* dst = (float*)c_base + r * p.ldc + n;
-            *(f32x4*)dst = EPI == EPI_STORE_F32 ? acc[i][2 * P] : sc * acc[i][2 * P];
-            *(f32x4*)(dst + 4) = EPI == EPI_STORE_F32 ? acc[i][2 * P + 1] : sc * acc[i][2 * P + 1];
+          } else {                                               // EPI_ROWSCALE_F32, EPI_STORE_F32, EPI_SEVERAL
+            float* dst = (float*)c_base + r * (SEVERAL ? q_mm.ldc : p.ldc) + n;
+            *(f32x4*)dst = EPI != EPI_ROWSCALE_F32 ? MOEP_OUT(0) : sc * acc[i][2 * P];
+            *(f32x4*)(dst + 4) = EPI != EPI_ROWSCALE_F32 ? MOEP_OUT(1) : sc * acc[i][2 * P + 1];
           }
         }
       }
@@ -597,6 +650,7 @@ __device__ __forceinline__ void gemm_body() {
     decode(L_mm, tm, tn, e_mm);
   }
   __builtin_amdgcn_s_waitcnt(0x0070);   // the re-reads still in flight target this workgroup's LDS
+#undef MOEP_OUT
 #undef MOEP_BUFFER_LOAD
 #undef MOEP_LOAD_A
 #undef MOEP_LOAD_B

@@ -7,7 +7,8 @@
 namespace moep {
 
 int allow_train_gemms() {
-  for (auto allow : {allow_lds<EPI_SWIGLU_KEEP, false, true>, allow_lds<EPI_STORE_F32, false, false>, allow_lds<EPI_STORE_F32, false, true>})
+  for (auto allow : {allow_lds<EPI_SWIGLU_KEEP, false, true>, allow_lds<EPI_STORE_F32, false, false>, allow_lds<EPI_STORE_F32, false, true>,
+                     allow_lds<EPI_SEVERAL, false, false>})
     if (int st = allow()) return st;
   return MOEP_OK;
 }
@@ -21,6 +22,42 @@ int launch_gemm_bf16_train(const PackedGemmArgs& g, hipStream_t s, const char* n
   if (g.epilogue == EPI_SWIGLU_KEEP && g.b_row_major) return launch<EPI_SWIGLU_KEEP, false, true>(k, s);
   if (g.epilogue == EPI_STORE_F32) return g.b_row_major ? launch<EPI_STORE_F32, false, true>(k, s) : launch<EPI_STORE_F32, false, false>(k, s);
   return fail(MOEP_EINVAL, "%s: unsupported epilogue %d", name, g.epilogue);
+}
+
+int launch_gemm_bf16_several(const PackedProduct* q, int n, hipStream_t s, const char* name) {
+  if (n < 1 || n > SEVERAL_MAX) return fail(MOEP_EINVAL, "%s: %d GEMMs", name, n);
+  KArgs k = {};
+  int order[SEVERAL_MAX];
+  int64_t full = 0, rows = 0;
+  for (int i = 0; i < n; ++i) {
+    if (q[i].M <= 0 || q[i].N <= 0 || q[i].N % 32 || q[i].ranges < 1 || q[i].K <= 0 || q[i].K % ((int64_t)64 * q[i].ranges))
+      return fail(MOEP_EINVAL, "%s: M=%lld, N=%d, K=%d in %d ranges", name, (long long)q[i].M, q[i].N, q[i].K, q[i].ranges);
+    if (((uintptr_t)q[i].A | (uintptr_t)q[i].B | (uintptr_t)q[i].C) & 15) return fail(MOEP_EUNSUPPORTED, "%s: operands must be 16-byte aligned", name);
+    full += ceil_div(q[i].M, 256) * ceil_div(q[i].N, GEMM_BN_STORE) * q[i].ranges;
+    if (q[i].M > rows) rows = q[i].M;
+    int at = i;
+    for (; at > 0 && q[order[at - 1]].K / q[order[at - 1]].ranges < q[i].K / q[i].ranges; --at) order[at] = order[at - 1];
+    order[at] = i;
+  }
+  const bool half = half_width_pays(full);
+  int64_t tiles = 0;
+  for (int i = 0; i < n; ++i) {
+    const PackedProduct& g = q[order[i]];
+    KProblem& d = k.several[i];
+    d.A = (const char*)g.A; d.B = (const char*)g.B; d.C = g.C;
+    d.M = g.M; d.ldc = g.N; d.N = g.N; d.c_range_bytes = g.M * g.N * 4; d.f32 = g.ranges > 1;
+    d.wide_nsl = g.K / 32; d.nsl = d.wide_nsl / g.ranges;
+    d.m_tiles = (int)ceil_div(g.M, 256); d.n_tiles = (int)ceil_div(g.N, gemm_tile_columns(false, half));
+    tiles += (int64_t)d.m_tiles * d.n_tiles * g.ranges;
+    if (tiles >= (int64_t)1 << 31 || g.ranges >= 1 << 28) return fail(MOEP_EUNSUPPORTED, "%s: too many tiles", name);
+    d.end = (uint32_t)tiles;
+  }
+  k.problems = n;
+  k.m_tiles = (int)tiles; k.n_tiles = 1; k.experts = 1;      // (what the grid is made from)
+  k.half_width = half ? 1 : 0;
+  k.row_groups = gemm_row_groups(rows);
+  Timed t(name, s);
+  return launch<EPI_SEVERAL, false, false>(k, s);
 }
 
 }  // namespace moep

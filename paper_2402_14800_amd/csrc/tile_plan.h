@@ -87,4 +87,36 @@ constexpr int64_t k_ranges(int64_t tiles, int64_t room, int64_t units, int64_t l
   return n;
 }
 
+// The three products that end an expert's backward pass (dx; dW1 and dW3; dW2), as one launch where they are so small that one tile per
+// compute unit is about what they come to: each is cut along its K so that a tile takes about the same number of steps.  Steps are
+// 64 of K.  The price of a cut: the steps of the first compute unit, which the longest tiles are dealt to, TILE_STEPS more a tile, and the
+// write and read of the ranges' sums at SUM_BYTES a step; tiles of half the width, while they fit one round, at 10/16.
+struct BackwardCut { bool together; int64_t dx_ranges, t_ranges; };
+constexpr int64_t TOGETHER_MAX_STEPS = 64, TILE_STEPS = 6, SUM_BYTES = 1750000;
+constexpr BackwardCut cut_backward(int64_t T, int64_t H, int64_t F) {
+  const int64_t mt = (T + 255) / 256, mh = (H + 255) / 256, mf = (F + 255) / 256, dx_units = F / 32, t_units = (T + 63) / 64;
+  const int64_t steps = (mt * mh * dx_units + 3 * mf * mh * t_units + 255) / 256;
+  BackwardCut best = {steps <= TOGETHER_MAX_STEPS, 1, 1};
+  int64_t price = -1;
+  for (int64_t each = 8; best.together && each <= 2 * TOGETHER_MAX_STEPS; ++each) {
+    int64_t dx = dx_units / each, t = t_units / each;
+    if (dx < 1) dx = 1;
+    if (t < 1) t = 1;
+    while (dx_units % dx) --dx;
+    const int64_t dx_tiles = mt * mh * dx, t_tiles = 3 * mf * mh * t, dx_steps = dx_units / dx, t_steps = (t_units + t - 1) / t;
+    const int64_t first = dx_steps >= t_steps ? dx_tiles : t_tiles, tiles = dx_tiles + t_tiles;
+    const int64_t longer = dx_steps >= t_steps ? dx_steps : t_steps, shorter = dx_steps >= t_steps ? t_steps : dx_steps;
+    const int64_t long_rounds = (first + 255) / 256, rounds = (tiles + 255) / 256;
+    int64_t p = 16 * (long_rounds * longer + (rounds - long_rounds) * shorter + rounds * TILE_STEPS);
+    if (half_width_pays(tiles)) p = p * 10 / 16;
+    p += 16 * 8 * ((dx > 1 ? dx * T * H : 0) + (t > 1 ? 3 * t * F * H : 0)) / SUM_BYTES;
+    if (price < 0 || p < price) {
+      price = p;
+      best.dx_ranges = dx;
+      best.t_ranges = t;
+    }
+  }
+  return best;
+}
+
 }  // namespace moep
