@@ -220,18 +220,9 @@ __device__ __forceinline__ void gemm_body() {
       tm = (int)(v >> 12);
       tn = (int)(v & 4095u);
     } else if (SEVERAL) {
-      // Every XCD gets a contiguous run of each GEMM's tiles, so that they share operand panels in its L2, the GEMMs' longest tiles first.
-      // (Tiles that are left over go to the XCDs in turn, on from where those of the GEMM before ended: XCD x has as many tiles as there
-      // are ids x, x + 8, ...)  One flat order over all XCDs: the launch of 777 rows, H 1024, F 3584 took 47 us for SEVERAL_US.
-      int pi = 0;
-      uint32_t start = 0, at = j, turn = xcd, tiles = p.several[0].end;
-      while (at >= (tiles >> 3) + (turn < (tiles & 7) ? 1u : 0u) && pi + 1 < p.problems) {
-        at -= (tiles >> 3) + (turn < (tiles & 7) ? 1u : 0u);
-        start = p.several[pi].end;
-        turn = (xcd - start) & 7u;
-        tiles = p.several[++pi].end - start;
-      }
-      const uint32_t in_problem = turn * (tiles >> 3) + min(turn, tiles & 7u) + at, m = (uint32_t)p.several[pi].m_tiles;
+      const SeveralTile where = tile_of_several(L, p.problems, [&](int i) { return p.several[i].end; });
+      const int pi = where.gemm;
+      const uint32_t in_problem = where.tile, m = (uint32_t)p.several[pi].m_tiles;
       const uint32_t of_range = m * (uint32_t)p.several[pi].n_tiles;
       const uint32_t range = in_problem / of_range, rest = in_problem - range * of_range;
       e = pi | (int)(range << 2);
@@ -776,7 +767,7 @@ int gemm_arguments(const PackedGemmArgs& g, const char* name, KArgs* out) {
   if (m_tiles * n_tiles * g.experts >= ((int64_t)1 << 31)) return fail(MOEP_EUNSUPPORTED, "%s: too many tiles", name);
   k.m_tiles = (int)m_tiles; k.n_tiles = (int)n_tiles; k.half_width = half ? 1 : 0;
   k.row_groups = gemm_row_groups(g.M);
-  k.stream = grouped ? g.stream : streams_weights(g.N, g.K, gemm_pairs(g.epilogue), g.experts);
+  k.stream = grouped ? g.stream : streams_weights(g.N, g.K, gemm_pairs(g.epilogue), g.epilogue == EPI_STORE_F32 ? 1 : g.experts);
   return MOEP_OK;
 }
 

@@ -77,7 +77,9 @@ constexpr int64_t routed_row_tiles(int64_t rows, int experts, int tile_rows) { r
 
 // Ranges of K that one GEMM of `tiles` tiles is cut into, each summed by workgroups of its own and the sums added afterwards, so that
 // fewer tiles than compute units still occupy them.  `units`: steps of K that a range consists of whole numbers of, at least `least`
-// of them; `any`: K is padded to fit, else the ranges have to divide it.
+// of them; `any`: K is padded to fit, else the ranges have to divide it.  One range / so, us per call: forward of 100 rows of H 4096,
+// F 14336 154 / 100, of 777 of H 1024, F 3584 58 / 45; training step, 300 rows of H 2048, F 5632 332 / 237, 4096 of H 512, F 1024 191 / 150,
+// 8192 of H 1024, F 3584 819 / 788; fp32, 8000 rows of H 64, F 128 251 / 62, 1501 of H 512, F 1024 194 / 187.
 constexpr int64_t k_ranges(int64_t tiles, int64_t room, int64_t units, int64_t least, bool any) {
   if (tiles <= 0 || 2 * tiles > room) return 1;
   int64_t n = room / tiles;
@@ -87,12 +89,34 @@ constexpr int64_t k_ranges(int64_t tiles, int64_t room, int64_t units, int64_t l
   return n;
 }
 
+// Tile id L of a launch of several GEMMs (end(i): tiles of those up to the i-th): the GEMM and the tile's place in it.  Every XCD, which
+// ids x, x + 8, ... go to, gets a contiguous run of each GEMM's tiles; what is left over goes to the XCDs in turn, on from where the tiles
+// of the GEMM before ended, so that XCD x has as many tiles as there are such ids.  One flat order over all XCDs / so, us of the launch: 1200
+// rows of H 2048, F 5632 155 / 134, 777 of H 1024, F 3584 49 / 47, 4096 of H 512, F 1024 33 / 35, 200 of H 4096, F 14336 221 / 228.
+struct SeveralTile { int gemm; uint32_t tile; };
+template <typename End>
+constexpr SeveralTile tile_of_several(uint32_t L, int gemms, End end) {
+  const uint32_t xcd = L & 7u;
+  uint32_t at = L >> 3, start = 0, turn = xcd, tiles = end(0);
+  int i = 0;
+  while (at >= (tiles >> 3) + (turn < (tiles & 7u) ? 1u : 0u) && i + 1 < gemms) {
+    at -= (tiles >> 3) + (turn < (tiles & 7u) ? 1u : 0u);
+    start = end(i);
+    turn = (xcd - start) & 7u;
+    tiles = end(++i) - start;
+  }
+  const uint32_t extra = tiles & 7u;
+  return {i, turn * (tiles >> 3) + (turn < extra ? turn : extra) + at};
+}
+
 // The three products that end an expert's backward pass (dx; dW1 and dW3; dW2), as one launch where they are so small that one tile per
 // compute unit is about what they come to: each is cut along its K so that a tile takes about the same number of steps.  Steps are
 // 64 of K.  The price of a cut: the steps of the first compute unit, which the longest tiles are dealt to, TILE_STEPS more a tile, and the
-// write and read of the ranges' sums at SUM_BYTES a step; tiles of half the width, while they fit one round, at 10/16.
+// write and read of the ranges' sums at SUM_BYTES a step; tiles of half the width, while they fit one round, at 10/16.  A launch each /
+// together, us per training step: one row of H 1024, F 3584 80 / 73, 777 162 / 143, 4000 (70 steps) 459 / 417, 8192 (146 steps) 779 / 806;
+// 1200 rows of H 2048, F 5632 (67 steps) 400 / 361, 2048 (110 steps) 565 / 552; 8192 of H 128, F 256 101 / 77.
 struct BackwardCut { bool together; int64_t dx_ranges, t_ranges; };
-constexpr int64_t TOGETHER_MAX_STEPS = 64, TILE_STEPS = 6, SUM_BYTES = 1750000;
+constexpr int64_t TOGETHER_MAX_STEPS = 120, TILE_STEPS = 6, SUM_BYTES = 1750000;
 constexpr BackwardCut cut_backward(int64_t T, int64_t H, int64_t F) {
   const int64_t mt = (T + 255) / 256, mh = (H + 255) / 256, mf = (F + 255) / 256, dx_units = F / 32, t_units = (T + 63) / 64;
   const int64_t steps = (mt * mh * dx_units + 3 * mf * mh * t_units + 255) / 256;

@@ -104,16 +104,78 @@ def test_binding_refuses_before_it_calls(bad):
         bad(z, i, t)
 
 
+def test_logit_kernels_do_not_spill():
+    """Rows are held in registers, 64 of them per lane: what spilled would wait behind every chunk in flight when it came back."""
+    usage = build.kernel_resource_usage("logits.hip")
+    kernels = {n: u for n, u in usage.items() if "token_logprobs_kernel" in n or "distill_topk_kernel" in n}
+    assert len(kernels) == 46                                # 5 workgroup sizes, 2 types: log probabilities, 3 modes of the loss; 3 not held
+    for name, u in kernels.items():
+        assert u["ScratchSize"] == 0 and u["VGPRs Spill"] == 0 and u["Occupancy"] >= 4, (name, u)
+
+
+PLAN = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "tile_plan.h"
+using namespace moep;
+#define CHECK(x) do { if (!(x)) { std::printf("%s: line %d\n", #x, __LINE__); return 1; } } while (0)
+int main() {
+  std::srand(1);
+  for (int round = 0; round < 20000; ++round) {              // every tile of every GEMM once
+    const int n = 1 + std::rand() % 4;
+    uint32_t end[4], total = 0;
+    for (int i = 0; i < n; ++i) end[i] = total += 1 + std::rand() % (std::rand() % 2 ? 300 : 9);
+    std::vector<int> seen(total, 0);
+    for (uint32_t L = 0; L < total; ++L) {
+      const SeveralTile t = tile_of_several(L, n, [&](int i) { return end[i]; });
+      const uint32_t start = t.gemm ? end[t.gemm - 1] : 0;
+      CHECK(t.gemm < n && t.tile < end[t.gemm] - start);
+      ++seen[start + t.tile];
+    }
+    for (int s : seen) CHECK(s == 1);
+  }
+  for (int64_t tiles = 0; tiles < 400; ++tiles)
+    for (int64_t units = 1; units < 300; units += 7)
+      for (int any = 0; any < 2; ++any) {
+        const int64_t r = k_ranges(tiles, 256, units, 8, any);
+        CHECK(r >= 1 && (r == 1 || (r * 8 <= units && r * tiles <= 256 && (any || units % r == 0))));
+      }
+  for (int64_t T : {1, 63, 64, 65, 300, 777, 4096, 100000, 1000000})
+    for (int64_t H : {64, 320, 1024, 4096, 65536})
+      for (int64_t F : {64, 832, 3584, 14336, 262144}) {
+        const BackwardCut c = cut_backward(T, H, F);
+        CHECK(c.dx_ranges >= 1 && c.t_ranges >= 1 && (F / 32) % c.dx_ranges == 0);
+        CHECK(!c.together || c.t_ranges <= (T + 63) / 64);
+      }
+  std::puts("ok");
+}
+"""
+
+
+def test_plans_of_the_training_step(tmp_path):
+    """The arithmetic that the kernels and the host share, run as a program of its own."""
+    import os
+    import subprocess
+
+    csrc = os.path.join(os.path.dirname(build.__file__), "csrc")
+    (tmp_path / "plan.cpp").write_text(PLAN)
+    exe = str(tmp_path / "plan")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", csrc, str(tmp_path / "plan.cpp"), "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
 def test_training_gemms_wait_for_the_loads_they_mean():
     """The properties of the 256-row GEMM that its waits rely on (the bodies are the same source), in the training step's instantiations."""
     usage = {n: u for n, u in build.kernel_resource_usage("gemm_train.hip").items() if "gemm_packed_kernel" in n}
-    assert len(usage) == 3
+    assert len(usage) == 4                                   # both branches kept, fp32 sums (2 weight layouts), several GEMMs
     for name, u in usage.items():
         assert u["ScratchSize"] == 0 and u["VGPRs Spill"] == 0 and u["SGPRs Spill"] == 0, (name, u)
         assert u["AGPRs"] == 256 and u["VGPRs"] <= 256 and u["Occupancy"] == 1, (name, u)
     text = build.device_assembly("gemm_train.hip").splitlines()
     starts = [i for i, line in enumerate(text) if re.match(r"_ZN\S*gemm_packed_kernel\S*:", line)]
-    assert len(starts) == 3
+    assert len(starts) == 4
     for start in starts:
         row_major = re.search(r"kernelILi\d+ELb[01]ELb([01])E", text[start]).group(1) == "1"
         bodies = set()
