@@ -590,12 +590,16 @@ def _logit_rows(logits):
     return T, V, max(step, V) if T > 1 else V
 
 
-def _vector(t, shape, dtype, like, what):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+def _beside(t, shape, dtype, index: int, what: str):
+    """Checks an operand that goes with the logits on GPU `index`."""
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
-    if t.get_device() != like.get_device() or not t.is_contiguous():
+    if t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous and on the logits' GPU")
-    return t
+
+
+# (sizes as plain numbers: torch.empty takes 0.4 us longer for a tuple, and these calls allocate several small tensors)
+_empty = torch.empty
 
 
 def moe_token_logprobs(logits, tokens, top: int = 0):
@@ -603,22 +607,32 @@ def moe_token_logprobs(logits, tokens, top: int = 0):
     (negative: none given).  Rows of logits may be views into longer rows."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
-    _vector(tokens, (T,), torch.int64, logits, "tokens")
     dev = logits.device
-    logprob, entropy = torch.empty((T,), dtype=torch.float32, device=dev), torch.empty((T,), dtype=torch.float32, device=dev)
-    top_logprob = torch.empty((T, max(top, 0)), dtype=torch.float32, device=dev)
-    top_ids = torch.empty((T, max(top, 0)), dtype=torch.int32, device=dev)
-    _check(_lib.moe_token_logprobs(_ptr(logits), ld, _ptr(tokens), T, V, dt, top, _ptr(logprob), _ptr(entropy),
-                                   _ptr(top_logprob), _ptr(top_ids), _stream(dev)))
+    _beside(tokens, (T,), torch.int64, dev.index, "tokens")
+    columns = max(top, 0)
+    logprob, entropy = _empty(T, dtype=torch.float32, device=dev), _empty(T, dtype=torch.float32, device=dev)
+    top_logprob = _empty(T, columns, dtype=torch.float32, device=dev)
+    top_ids = _empty(T, columns, dtype=torch.int32, device=dev)
+    _check(_lib.moe_token_logprobs(logits.data_ptr(), ld, tokens.data_ptr(), T, V, dt, top, logprob.data_ptr(), entropy.data_ptr(),
+                                   top_logprob.data_ptr(), top_ids.data_ptr(), _raw_stream(dev.index)))
     return logprob, entropy, top_logprob, top_ids
 
 
 def _gradient_rows(logits, grad, T: int, V: int):
     if grad is None:
-        grad = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        return _empty(T, V, dtype=logits.dtype, device=logits.device), V
     if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.get_device() != logits.get_device():
         raise ValueError("the gradient must be like the logits")
     return grad, _logit_rows(grad)[2]
+
+
+def _alternatives(ids, teacher, T: int, index: int) -> int:
+    if ids.dim() != 2:
+        raise ValueError("ids must be [T, K]")
+    K = ids.shape[1]
+    _beside(ids, (T, K), torch.int32, index, "ids")
+    _beside(teacher, (T, K), torch.float32, index, "teacher")
+    return K
 
 
 def moe_distill_topk(logits, ids, teacher, temperature: float = 1.0, weights=None, gradient: bool = False, out=None):
@@ -627,16 +641,14 @@ def moe_distill_topk(logits, ids, teacher, temperature: float = 1.0, weights=Non
     `out` if given (which may be `logits` itself)."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
-    K = ids.shape[1] if ids.dim() == 2 else 0
-    _vector(ids, (T, K), torch.int32, logits, "ids")
-    _vector(teacher, (T, K), torch.float32, logits, "teacher")
-    if weights is not None:
-        _vector(weights, (T,), torch.float32, logits, "weights")
     dev = logits.device
-    loss, stats = torch.empty((T,), dtype=torch.float32, device=dev), torch.empty((T, 2), dtype=torch.float32, device=dev)
+    K = _alternatives(ids, teacher, T, dev.index)
+    if weights is not None:
+        _beside(weights, (T,), torch.float32, dev.index, "weights")
+    loss, stats = _empty(T, dtype=torch.float32, device=dev), _empty(T, 2, dtype=torch.float32, device=dev)
     grad, ld_grad = _gradient_rows(logits, out, T, V) if gradient else (None, 0)
-    _check(_lib.moe_distill_topk(_ptr(logits), ld, _ptr(ids), _ptr(teacher), T, V, K, dt, temperature, _ptr(weights),
-                                 _ptr(loss), _ptr(stats), _ptr(grad), ld_grad, _stream(dev)))
+    _check(_lib.moe_distill_topk(logits.data_ptr(), ld, ids.data_ptr(), teacher.data_ptr(), T, V, K, dt, temperature, _ptr(weights),
+                                 loss.data_ptr(), stats.data_ptr(), _ptr(grad), ld_grad, _raw_stream(dev.index)))
     return (loss, stats, grad) if gradient else (loss, stats)
 
 
@@ -644,14 +656,14 @@ def moe_distill_topk_backward(logits, ids, teacher, stats, grad_loss, temperatur
     """The gradient [T,V] by the logits, from moe_distill_topk's stats and the upstream gradient [T] fp32 of its loss."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
-    K = ids.shape[1] if ids.dim() == 2 else 0
-    _vector(ids, (T, K), torch.int32, logits, "ids")
-    _vector(teacher, (T, K), torch.float32, logits, "teacher")
-    _vector(stats, (T, 2), torch.float32, logits, "stats")
-    _vector(grad_loss, (T,), torch.float32, logits, "grad_loss")
+    dev = logits.device
+    K = _alternatives(ids, teacher, T, dev.index)
+    _beside(stats, (T, 2), torch.float32, dev.index, "stats")
+    _beside(grad_loss, (T,), torch.float32, dev.index, "grad_loss")
     grad, ld_grad = _gradient_rows(logits, out, T, V)
-    _check(_lib.moe_distill_topk_backward(_ptr(logits), ld, _ptr(ids), _ptr(teacher), _ptr(stats), _ptr(grad_loss), T, V, K,
-                                          dt, temperature, _ptr(grad), ld_grad, _stream(logits.device)))
+    _check(_lib.moe_distill_topk_backward(logits.data_ptr(), ld, ids.data_ptr(), teacher.data_ptr(), stats.data_ptr(),
+                                          grad_loss.data_ptr(), T, V, K, dt, temperature, grad.data_ptr(), ld_grad,
+                                          _raw_stream(dev.index)))
     return grad
 
 
