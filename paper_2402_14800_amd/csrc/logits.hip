@@ -70,7 +70,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // A row seen as 16-byte chunks from the boundary at or before its first element: chunk c holds elements c N - lead .. + N - 1,
 // of which those within [0, V) are the row's.  Rows need no alignment beyond their elements'.  A chunk that reaches beyond the row on
 // either side is loaded whole where that stays between the first row's first element and the last row's last, and cut to the row in
-// registers; only the first row's first chunk and the last row's last one are put together element by element.
+// registers (what it brought of the neighbours, who may be writing theirs, goes unused); only the first row's first chunk and the last row's
+// last one are put together element by element.
 template <typename S>
 struct Row {
   static constexpr int N = Elements<S>::N;
@@ -297,7 +298,7 @@ template <int B>
 struct SearchSpace {
   // Chunks with an element that reaches the threshold: each wavefront's in the order it met them, and where they begin in the row.
   // (one wavefront gets less room, so that twenty of them fit a compute unit)
-  static constexpr int HITS = B == 64 ? 128 : B >= 1024 ? 48 : 512 / (B / 64), CANDIDATES = B == 64 ? 256 : 512;
+  static constexpr int HITS = B == 64 ? 128 : 512 / (B / 64), CANDIDATES = B == 64 ? 256 : 512;
   u32x4 hit[B / 64 * HITS];
   int hit_at[B / 64 * HITS];
   unsigned threshold_of[2][B / 64];          // the wavefronts', of this tile and the one before
@@ -788,23 +789,25 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
 }
 
 // Threads per row of a loss: the fewest whose registers hold it whole, so that many rows are in flight on a compute unit at different
-// points of their way, and fewer barriers stop them; few rows get more threads, since there is nothing else for the compute units to
-// do.  0: none hold it.
+// points of their way, and fewer barriers stop them.  us, 4096 rows, loss and gradient, 64 / 128 / 256 / 512 / 1024 threads: V = 4096 bf16 (512
+// chunks) 19 / 21 / 26 / 46 / 93; 8000 (1000) 28 / 31 / 32 / 51 / 98; 16000 (2000) - / 55 / 50 / 68 / 115; 24000 (3000) - / - / 81 / 87 / 135; 32000 (4000)
+// - / - / 110 / 104 / 158 (1000 rows: 25 / 30 / 41); 65000 (8125) - / - / - / 207 / 233; 131072 (16384) held by 1024 412, not held 511.  Few rows
+// get more threads, since there is nothing else for the compute units to do: 33 rows of 1003 fp32 logits 7.9 us with 64 threads, 6.6
+// with 256; one of 32000 bf16 9.7 with 256, 8.4 with 512.  0: none hold it.
 int threads_to_hold(int64_t T, int64_t chunks) {
   if (chunks > 1024 * NC) return 0;
-  if (T <= 512 && chunks > 256) return 1024;
+  if (T <= 512) return chunks <= 512 ? 256 : chunks <= 512 * NC ? 512 : 1024;
   if (chunks <= 64 * NC) return 64;
   if (chunks <= 128 * 12) return 128;                        // (of 16 that there is room for)
   if (chunks <= 256 * (T < 2048 ? NC : 14)) return 256;
   return chunks <= 512 * NC ? 512 : 1024;
 }
-// Threads per row of log probabilities, which need not be held: one wavefront where that holds the row, else 256, of few rows more (and at
-// most two tiles then).
+// Threads per row of log probabilities, which need not be held: one wavefront where that holds a row of many, else 256, or 512 where few
+// rows have more than a tile.  us, 64 / 256 / 512 / 1024 threads: 8192 rows of 4096 bf16, K = 5 21 / 46 / 95 / 214; 8192 of 32000, K = 64 122 / 115 /
+// 176 / 330; 777 of 50001 fp32 56 / 43 / 38 / 54; 300 of 131072 bf16 79 / 34 / 32 / 40; one of 32000 - / 9.0 / 9.3 / 10.8, of 131072 - / 23.3 / 17.6 / 16.9.
 int threads_to_read(int64_t T, int64_t chunks) {
   if (chunks <= 64 * NC && T > 2048) return 64;
-  for (int b : {256, 512})
-    if ((T * b >= 150000 && (T >= 1024 || chunks <= 2 * b * NC)) || chunks <= b) return b;
-  return 1024;
+  return T >= 1024 || chunks <= 256 * NC ? 256 : 512;
 }
 // Chunks of a row at most: its elements from the 16-byte boundary before it on, which is as far for every row where `ld` is whole chunks.
 int64_t most_chunks(const void* logits, int64_t ld, int64_t V, moep_dtype dt) {
@@ -818,8 +821,7 @@ void with_threads(int threads, F launch) {
     case 64: launch(std::integral_constant<int, 64>{}); break;
     case 128: launch(std::integral_constant<int, 128>{}); break;
     case 256: launch(std::integral_constant<int, 256>{}); break;
-    case 512: launch(std::integral_constant<int, 512>{}); break;
-    default: launch(std::integral_constant<int, 1024>{});
+    default: launch(std::integral_constant<int, 512>{});
   }
 }
 
@@ -832,20 +834,37 @@ int check_rows(const char* who, int64_t T, int64_t V, moep_dtype dt, const void*
   return MOEP_OK;
 }
 
+// Rows of a launch: a grid has fewer than 2^32 threads.
+constexpr int64_t LAUNCH_ROWS = (int64_t)1 << 22;
+
 template <int MODE>
-int launch_distill(const DistillArgs& p, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
-  const int64_t chunks = most_chunks(p.logits, p.ld, p.V, dt);
+int launch_distill(const DistillArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
+  const int64_t chunks = most_chunks(whole.logits, whole.ld, whole.V, dt);
   const int threads = threads_to_hold(T, chunks);
   Timed timed(name, s);
-  auto with = [&](auto b, auto held) {
-    constexpr int B = decltype(b)::value;
-    constexpr bool HELD = decltype(held)::value;
-    if (dt == MOEP_BF16) hipLaunchKernelGGL((distill_topk_kernel<uint16_t, B, MODE, HELD>), dim3((unsigned)T), dim3(B), 0, s, p);
-    else hipLaunchKernelGGL((distill_topk_kernel<float, B, MODE, HELD>), dim3((unsigned)T), dim3(B), 0, s, p);
-  };
-  if (threads) with_threads(threads, [&](auto b) { with(b, std::true_type{}); });
-  else with(std::integral_constant<int, 1024>{}, std::false_type{});
-  MOEP_HIP(hipGetLastError());
+  for (int64_t t = 0; t < T; t += LAUNCH_ROWS) {
+    DistillArgs p = whole;
+    p.T = T - t < LAUNCH_ROWS ? T - t : LAUNCH_ROWS;
+    const int64_t size = (int64_t)dtype_size(dt);
+    p.logits = (const char*)whole.logits + t * whole.ld * size;
+    p.ids = whole.ids + t * whole.K;
+    p.teacher = whole.teacher + t * whole.K;
+    if (p.weights) p.weights += t;
+    if (p.loss) p.loss += t;
+    p.stats += 2 * t;
+    if (p.grad) p.grad = (char*)whole.grad + t * whole.ld_grad * size;
+    auto with = [&](auto b, auto held) {
+      constexpr int B = decltype(b)::value;
+      constexpr bool HELD = decltype(held)::value;
+      if (dt == MOEP_BF16) hipLaunchKernelGGL((distill_topk_kernel<uint16_t, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
+      else hipLaunchKernelGGL((distill_topk_kernel<float, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
+    };
+    constexpr auto most = std::integral_constant<int, 1024>{};
+    if (!threads) with(most, std::false_type{});
+    else if (threads == 1024) with(most, std::true_type{});
+    else with_threads(threads, [&](auto b) { with(b, std::true_type{}); });
+    MOEP_HIP(hipGetLastError());
+  }
   return MOEP_OK;
 }
 
@@ -871,17 +890,21 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
   if (T == 0) return MOEP_OK;
   if (!logits || !tokens || !logprob || !entropy) return fail(MOEP_EINVAL, "%s: NULL logits, tokens, logprob or entropy", who);
   if (K > 0 && (!top_logprob || !top_ids)) return fail(MOEP_EINVAL, "%s: NULL top_logprob or top_ids", who);
-  LogprobArgs p = {logits, ld, T, (int)V, tokens, K, logprob, entropy, top_logprob, top_ids};
   hipStream_t s = (hipStream_t)hip_stream;
   int threads = threads_to_read(T, most_chunks(logits, ld, V, dt));
   if (threads == 64 && K > 32) threads = 128;                // (a threshold from few more than K threads lets too many through)
   Timed timed("token_logprobs", s);
-  with_threads(threads, [&](auto b) {
-    constexpr int B = decltype(b)::value;
-    if (dt == MOEP_BF16) hipLaunchKernelGGL((token_logprobs_kernel<uint16_t, B>), dim3((unsigned)T), dim3(B), 0, s, p);
-    else hipLaunchKernelGGL((token_logprobs_kernel<float, B>), dim3((unsigned)T), dim3(B), 0, s, p);
-  });
-  MOEP_HIP(hipGetLastError());
+  for (int64_t t = 0; t < T; t += LAUNCH_ROWS) {
+    const int64_t rows = T - t < LAUNCH_ROWS ? T - t : LAUNCH_ROWS;
+    LogprobArgs p = {(const char*)logits + t * ld * (int64_t)dtype_size(dt), ld, rows, (int)V, tokens + t, K, logprob + t, entropy + t,
+                     K ? top_logprob + t * K : nullptr, K ? top_ids + t * K : nullptr};
+    with_threads(threads, [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      if (dt == MOEP_BF16) hipLaunchKernelGGL((token_logprobs_kernel<uint16_t, B>), dim3((unsigned)rows), dim3(B), 0, s, p);
+      else hipLaunchKernelGGL((token_logprobs_kernel<float, B>), dim3((unsigned)rows), dim3(B), 0, s, p);
+    });
+    MOEP_HIP(hipGetLastError());
+  }
   return MOEP_OK;
 }
 

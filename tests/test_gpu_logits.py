@@ -134,6 +134,25 @@ def test_logprobs_beyond_32_bit_offsets():
     assert abs(float(lp[-1]) - float(rlp)) <= ABS
 
 
+def test_more_rows_than_a_launch_has():
+    T, V = (1 << 22) + 1001, 3
+    z = make_logits(T, V, torch.bfloat16, seed=6)
+    tokens = torch.arange(T, device=DEV) % V
+    lp, ent, tlp, ids = pkg.moe_token_logprobs(z, tokens, 2)
+    want = torch.log_softmax(z.double(), 1)
+    assert float((lp - want.gather(1, tokens[:, None])[:, 0]).abs().max()) <= ABS
+    assert float((tlp[:, 0] - want.max(1).values).abs().max()) <= ABS
+    teacher = torch.zeros((T, 1), device=DEV)
+    alternative = tokens[:, None].to(torch.int32).contiguous()
+    loss, stats, grad = pkg.moe_distill_topk(z, alternative, teacher, gradient=True)
+    assert float((loss + want.gather(1, tokens[:, None])[:, 0]).abs().max()) <= 4 * ABS
+    back = pkg.moe_distill_topk_backward(z, alternative, teacher, stats, torch.ones(T, device=DEV))
+    ref = want.exp()
+    ref[torch.arange(T, device=DEV), tokens] -= 1
+    for g in (grad, back):
+        assert float((g.double() - ref).abs().max()) <= 2.0 ** -8
+
+
 # ---------------------------------------------------------------- distillation
 def make_teacher(z, K, seed):
     g = torch.Generator().manual_seed(seed)
