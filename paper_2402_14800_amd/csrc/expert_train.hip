@@ -84,6 +84,8 @@ struct TransposeArgs {
   unsigned rows;                             // row blocks
 };
 
+// Reads and writes each matrix once: the two gate/up weights and the down weight of 4096 x 14336 with 8192 rows of tokens and of dy
+// take 193 us, 5.4 TB/s, the rate of a copy.  Six waves a SIMD cover a block's eight loads.
 template <typename S>
 __global__ __launch_bounds__(256, 6) void transpose_kernel(Jobs<TransposeArgs> jobs) {
   constexpr int N = N_OF<S>;
@@ -130,47 +132,70 @@ __device__ __forceinline__ u32x4 rounded(const float (&x)[N_OF<S>]) {
 }
 
 // Reads 12 bytes an element (dh, g, u in fp32: rounded to bf16 before this pass they would leave the gradients with twice the error of
-// one rounding) and writes five chunks' worth: da, db as the A operand of dx, da, db, h along the tokens.
-template <typename S>
+// one rounding) and writes five chunks' worth: da, db as the A operand of dx, da, db, h along the tokens.  Bound by that, 22 bytes an
+// element of bf16: 8192 x 14336 at 4.9 TB/s.  ROWS of a thread's block are asked for together, and without branches between them (rows beyond
+// the last one repeat it, and are cleared): with a branch for each row and its stores in front of the next row's loads it was 4.2 TB/s.
+// All rows in flight take 256 registers, one wave a SIMD; held to two waves it spills (597 us instead of 524).
+// SUMMED: dh comes in several parts; few rows then, whose loads are all that the launch waits for (8 rows: 24 to 30 us, now 19 to 21).
+template <typename S, bool SUMMED>
 __global__ __launch_bounds__(256) void branch_gradients_kernel(BranchArgs p) {
-  constexpr int N = N_OF<S>;
+  constexpr int N = N_OF<S>, ROWS = SUMMED ? 4 : 2;
   const Place<S> at(blockIdx.x, blockIdx.y);
   if (at.c0 >= p.F || at.r0 >= p.da_t.K) return;
   u32x4 a[N], b[N], h[N], out[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    a[i] = b[i] = h[i] = u32x4{0, 0, 0, 0};
-    const int64_t t = at.r0 + i;
-    if (t < p.T) {
-      const int64_t e = t * p.F + at.c0;
-      float dh[N], g[N], u[N], xa[N], xb[N], xh[N];
+  for (int i0 = 0; i0 < N; i0 += ROWS) {
+    float dh[ROWS][N], g[ROWS][N], u[ROWS][N];
+    auto row = [&](int i) {
+      const int64_t t = at.r0 + i0 + i;
+      return (t < p.T ? t : p.T - 1) * p.F + at.c0;
+    };
+    auto load = [&](const float* from, int64_t e, float (&to)[N]) {
 #pragma unroll
-      for (int j = 0; j < N; j += 4) {
-        *(f32x4*)(dh + j) = *(const f32x4*)(p.dh + e + j);
-        *(f32x4*)(g + j) = *(const f32x4*)(p.g + e + j);
-        *(f32x4*)(u + j) = *(const f32x4*)(p.u + e + j);
+      for (int j = 0; j < N; j += 4) *(f32x4*)(to + j) = *(const f32x4*)(from + e + j);
+    };
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      load(p.dh, row(i), dh[i]);
+      load(p.g, row(i), g[i]);
+      load(p.u, row(i), u[i]);
+    }
+    if (SUMMED)
+#pragma unroll 2
+      for (int q = 1; q < p.parts; ++q) {
+        float x[ROWS][N];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) load(p.dh + q * p.part_stride, row(i), x[i]);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) dh[i][j] += x[i][j];
       }
-      for (int q = 1; q < p.parts; ++q)
 #pragma unroll
-        for (int j = 0; j < N; j += 4) {
-          const f32x4 x = *(const f32x4*)(p.dh + q * p.part_stride + e + j);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) dh[j + v] += x[v];
-        }
+    for (int i = 0; i < ROWS; ++i) {
+      float xa[N], xb[N], xh[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float s = 1.f / (1.f + __expf(-g[j])), silu = g[j] * s;
-        xa[j] = dh[j] * u[j] * (s * (1.f + g[j] * (1.f - s)));
-        xb[j] = dh[j] * silu;
-        xh[j] = silu * u[j];
+        const float s = 1.f / (1.f + __expf(-g[i][j])), silu = g[i][j] * s;
+        xa[j] = dh[i][j] * u[i][j] * (s * (1.f + g[i][j] * (1.f - s)));
+        xb[j] = dh[i][j] * silu;
+        xh[j] = silu * u[i][j];
       }
-      a[i] = rounded<S>(xa); b[i] = rounded<S>(xb); h[i] = rounded<S>(xh);
-      if (p.dab.p) {
-        *chunk_of<S>(p.dab, t, at.c0) = a[i];
-        *chunk_of<S>(p.dab, t, p.F + at.c0) = b[i];
-      }
+      const bool there = at.r0 + i0 + i < p.T;
+      const u32x4 zero = {0, 0, 0, 0};
+      a[i0 + i] = there ? rounded<S>(xa) : zero;
+      b[i0 + i] = there ? rounded<S>(xb) : zero;
+      h[i0 + i] = there ? rounded<S>(xh) : zero;
     }
   }
+  // (all stores after all loads: a row's would have to stay behind the stores of the row before)
+  if (p.dab.p)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at.r0 + i < p.T) {
+        *chunk_of<S>(p.dab, at.r0 + i, at.c0) = a[i];
+        *chunk_of<S>(p.dab, at.r0 + i, p.F + at.c0) = b[i];
+      }
   if (!p.da_t.p) return;
   auto put = [&](const u32x4 (&in)[N], const Operand& o) {
     transposed<S>(in, out);
@@ -247,8 +272,12 @@ int launch_gradients_of_branches(const float* dh, int parts, const float* g, con
   BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, dab, da_t, db_t, h_t};
   if (!p.da_t.p) p.da_t.K = T;
   Timed t("branch_gradients", s);
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(branch_gradients_kernel<uint16_t>, dim3((unsigned)row_blocks<uint16_t>(p.da_t.K), (unsigned)column_blocks(F)), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(branch_gradients_kernel<float>, dim3((unsigned)row_blocks<float>(p.da_t.K), (unsigned)column_blocks(F)), dim3(256), 0, s, p);
+  const dim3 grid((unsigned)(dt == MOEP_BF16 ? row_blocks<uint16_t>(p.da_t.K) : row_blocks<float>(p.da_t.K)), (unsigned)column_blocks(F));
+#define MOEP_BRANCH(S, SUMMED) hipLaunchKernelGGL((branch_gradients_kernel<S, SUMMED>), grid, dim3(256), 0, s, p)
+  if (dt == MOEP_BF16) { if (parts > 1) MOEP_BRANCH(uint16_t, true); else MOEP_BRANCH(uint16_t, false); }
+  else if (parts > 1) MOEP_BRANCH(float, true);
+  else MOEP_BRANCH(float, false);
+#undef MOEP_BRANCH
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
