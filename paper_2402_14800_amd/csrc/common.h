@@ -133,7 +133,7 @@ int launch_gemm_f32(const GemmArgs& g, hipStream_t s, const char* name);
 
 // ---- bf16 GEMM on packed operands (dense expert pass) ---------------------------------
 // Operands are re-laid out once into 16 KB blocks of 256 rows x 32 k-values (the layout is described in
-// gemm_bf16_packed.hip); EPI_SWIGLU writes its result as a packed A operand with K = N.
+// gemm_packed_kernel.h); EPI_SWIGLU writes its result as a packed A operand with K = N.
 struct PackedGemmArgs {
   const void* A = nullptr;       // packed A operand, indexed by M tile
   const void* B = nullptr;       // packed_b_bytes(N, K, epilogue == EPI_SWIGLU) per expert

@@ -48,8 +48,8 @@ __device__ __forceinline__ void transposed(const u32x4 (&in)[N_OF<S>], u32x4 (&o
   }
 }
 
-// Where a thread's block lies: workgroups walk 256 columns x N^2 rows, a wavefront 64 columns, 64 / N chunks side by side.
-template <typename S>
+// Where a thread's block lies: a workgroup's wavefronts each take 64 columns x N^2 rows, 64 / N chunks side by side.
+template <typename S, int THREADS = 256>
 struct Place {
   int64_t r0;
   int c0;
@@ -57,7 +57,7 @@ struct Place {
     constexpr int N = N_OF<S>, SIDE = 64 / N;
     const int lane = threadIdx.x & 63;
     r0 = (int64_t)row_block * (N * N) + (lane / SIDE) * N;
-    c0 = (int)column_block * 256 + (int)(threadIdx.x >> 6) * 64 + (lane % SIDE) * N;
+    c0 = (int)column_block * THREADS + (int)(threadIdx.x >> 6) * 64 + (lane % SIDE) * N;
   }
 };
 template <typename S> int64_t row_blocks(int64_t rows) { return ceil_div(rows, (int64_t)N_OF<S> * N_OF<S>); }
@@ -136,11 +136,14 @@ __device__ __forceinline__ u32x4 rounded(const float (&x)[N_OF<S>]) {
 // element of bf16: 8192 x 14336 at 4.9 TB/s.  ROWS of a thread's block are asked for together, and without branches between them (rows beyond
 // the last one repeat it, and are cleared): with a branch for each row and its stores in front of the next row's loads it was 4.2 TB/s.
 // All rows in flight take 256 registers, one wave a SIMD; held to two waves it spills (597 us instead of 524).
-// SUMMED: dh comes in several parts; few rows then, whose loads are all that the launch waits for (8 rows: 24 to 30 us, now 19 to 21).
+// SUMMED: dh comes in several parts; few rows then, whose loads are all that the launch waits for, and workgroups of one wave, which
+// reach more compute units: 8 rows of 4096 x 14336 20.7 us in workgroups of 256, 15.9 so; 8 of 1024 x 3584 18.7 / 12.6 (with its launch's
+// events).  8192 x 14336 in one part is 524 / 540.
+template <bool SUMMED> constexpr int BRANCH_THREADS = SUMMED ? 64 : 256;
 template <typename S, bool SUMMED>
-__global__ __launch_bounds__(256) void branch_gradients_kernel(BranchArgs p) {
+__global__ __launch_bounds__(BRANCH_THREADS<SUMMED>) void branch_gradients_kernel(BranchArgs p) {
   constexpr int N = N_OF<S>, ROWS = SUMMED ? 4 : 2;
-  const Place<S> at(blockIdx.x, blockIdx.y);
+  const Place<S, BRANCH_THREADS<SUMMED>> at(blockIdx.x, blockIdx.y);
   if (at.c0 >= p.F || at.r0 >= p.da_t.K) return;
   u32x4 a[N], b[N], h[N], out[N];
 #pragma unroll
@@ -272,8 +275,9 @@ int launch_gradients_of_branches(const float* dh, int parts, const float* g, con
   BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, dab, da_t, db_t, h_t};
   if (!p.da_t.p) p.da_t.K = T;
   Timed t("branch_gradients", s);
-  const dim3 grid((unsigned)(dt == MOEP_BF16 ? row_blocks<uint16_t>(p.da_t.K) : row_blocks<float>(p.da_t.K)), (unsigned)column_blocks(F));
-#define MOEP_BRANCH(S, SUMMED) hipLaunchKernelGGL((branch_gradients_kernel<S, SUMMED>), grid, dim3(256), 0, s, p)
+  const unsigned rows = (unsigned)(dt == MOEP_BF16 ? row_blocks<uint16_t>(p.da_t.K) : row_blocks<float>(p.da_t.K));
+#define MOEP_BRANCH(S, SUMMED)                                                                                                    \
+  hipLaunchKernelGGL((branch_gradients_kernel<S, SUMMED>), dim3(rows, (unsigned)ceil_div(F, BRANCH_THREADS<SUMMED>)), dim3(BRANCH_THREADS<SUMMED>), 0, s, p)
   if (dt == MOEP_BF16) { if (parts > 1) MOEP_BRANCH(uint16_t, true); else MOEP_BRANCH(uint16_t, false); }
   else if (parts > 1) MOEP_BRANCH(float, true);
   else MOEP_BRANCH(float, false);

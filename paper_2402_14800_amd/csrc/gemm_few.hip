@@ -1,7 +1,7 @@
 // bf16 expert GEMMs for FEW rows per expert (token generation, small batches): C = epilogue(A B^T), fp32 accumulate.
 //
 // With a few dozen rows per expert the work is a read of the weights: 2 flop per weight byte and row, so the launch
-// is bound by the memory from one row to about a hundred.  The 256-row tiles of gemm_bf16_packed.hip cannot reach that
+// is bound by the memory from one row to about a hundred.  The 256-row tiles of gemm_packed_kernel.h cannot reach that
 // bound: one token leaves most compute units without a tile (the down projection of 4096 x 14336 has 16 tiles per
 // expert, each a serial walk over 448 slices: 251 us for one token), and the padding rows are multiplied all the same.
 //
@@ -37,7 +37,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
-constexpr int SLICE = 256 * 64;     // bytes of one packed block (256 rows x 32 k), see gemm_bf16_packed.hip
+constexpr int SLICE = 256 * 64;     // bytes of one packed block (256 rows x 32 k), see gemm_packed_kernel.h
 constexpr int RING = 16384, DEEP_RING = 40960;   // LDS of a wavefront's load ring
 constexpr int DEEP_WAVES = 4;                    // wavefronts per compute unit up to which the deep ring is taken (they fit)
 // Wavefronts of a workgroup.  Four with the small ring: they read neighbouring column groups in step (16 tokens, packed: the

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void router_kernel(const void* __restrict__ x,
 // expert l % 16.  A token's sum depends on its own row and H only.  (Two tiles per wavefront sharing the
 // Wgate fragments, and 1 KB row-wise loads staged through LDS, both measured slower.)
 // PACK: the wavefront also writes its 16 rows of x in the blocked operand layout of the packed GEMM (see
-// gemm_bf16_packed.hip: tile of 256 rows, slice of 32 hidden units, row p of a block = 64 bytes whose 16-byte chunk c
+// gemm_packed_kernel.h: tile of 256 rows, slice of 32 hidden units, row p of a block = 64 bytes whose 16-byte chunk c
 // sits at position c ^ ((p >> 2) & 3)) -- the registers it feeds the MFMA with are exactly one row group of a block,
 // 1 KB of consecutive bytes per store -- so that the expert pass reads x once for both.  Row groups beyond T, up to
 // the end of the last tile, are filled with the last row (their products are never stored).
