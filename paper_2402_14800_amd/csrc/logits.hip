@@ -10,6 +10,9 @@
 // running maximum and sums (a rescale per 16 chunks), so the row is read without a barrier and joined once at its end.  Up to
 // 16 chunks of 16 bytes per thread stay in registers, so a row of up to 32768 bf16 logits on 256 threads is read from memory
 // once also where it is used again (the gradient, the search for the best); a longer one is walked tile by tile.
+// Time and bytes read and written: 1999 rows of 32000 bf16, K = 1 32.0 us (4.0 TB/s; the launch's beginning and its last workgroups cost 6 us
+// of it), 2048 of 131072, K = 64 115 us (4.7); loss and gradient of 4096 of 32000, K = 64 102 us (5.2, the rate of a copy), of 2048 of
+// 131072, K = 100 227 us (4.7); one row of 32000, K = 20 9 us, the workgroup's own way through it.
 // (Workgroups that stay and ask for their next row while they end the present one were slower everywhere, 1.1 to 1.7 times: loads and
 // stores return in order, so a row's first chunk waited for the stores before it. More workgroups than fit do the same without.)
 #include <type_traits>
