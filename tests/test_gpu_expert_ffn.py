@@ -142,6 +142,18 @@ def test_no_rows(dtype):
     assert y.shape == dx.shape == (0, 64) and not any(bool(w.any()) for w in dW)
 
 
+def test_step_beyond_32_bit_offsets():
+    T, H, F, n = 150016, 64, 14336, 300                       # T F is more than 2^31; dy is zero but for the last rows
+    x, W1, W3, W2, dy = make_block(T, H, F, torch.bfloat16, seed=9)
+    dy[:-n] = 0
+    (y, dx, *dW), gate_up = step(x, W1, W3, W2, dy)
+    ref, mag = reference(x[-n:], W1, W3, W2, dy[-n:])
+    check((y[-n:], dx[-n:], *dW), ref, mag, torch.bfloat16)
+    g = x[-n:].double() @ W1.double().T
+    assert float((gate_up[0, -n:].double() - g).abs().max()) <= H * 2.0 ** -24 * float((x[-n:].double().abs() @ W1.double().abs().T).max())
+    assert bool((dx[:-n] == 0).all())
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_steep_branches(dtype):
     """Gates far on either side of 0: the exponential overflows or vanishes, the gradients stay finite and right."""

@@ -265,6 +265,21 @@ def test_distillation_of_masked_and_empty_rows(V, dtype):
     check_gradient(grad, ref_distill(z, ids, teacher, 1.5, weights)[1], weights * 1.5, dtype)
 
 
+def test_distillation_beyond_32_bit_offsets():
+    V, T = 131072, 16400                                     # 2^31 elements and more, the gradient in the logits' own memory
+    z = torch.zeros((T, V), dtype=torch.bfloat16, device=DEV)
+    z[T - 1] = make_logits(1, V, torch.bfloat16, seed=5)[0]
+    ids = torch.tensor([[70001, 131071]], dtype=torch.int32, device=DEV).repeat(T, 1).contiguous()
+    teacher = torch.tensor([[1.0, 0.0]], device=DEV).repeat(T, 1).contiguous()
+    last = [0, T - 2, T - 1]                                 # (all rows but the last are alike)
+    rloss, ref = ref_distill(z[last], ids[last], teacher[last], 2.0)
+    loss, stats, grad = pkg.moe_distill_topk(z, ids, teacher, temperature=2.0, gradient=True, out=z)
+    assert grad.data_ptr() == z.data_ptr()
+    assert float((loss[last].double().cpu() - rloss).abs().max()) <= ABS * 2.0 ** 2 * 4 + 1e-6 * float(rloss.abs().max())
+    assert bool((loss[:-1] == loss[0]).all()) and all(torch.equal(grad[t], grad[0]) for t in range(16381, T - 1))
+    check_gradient(grad[last], ref, torch.full((3,), 2.0), torch.bfloat16)
+
+
 @pytest.mark.parametrize("V,K,tau", [(37, 5, 1.0), (1003, 20, 2.0), (9000, 64, 0.8)])
 def test_distillation_gradient_against_differences(V, K, tau):
     """<grad, d> = (L(z + e d) - L(z - e d)) / 2 e + O(e^2 L'''): with e = 2^-5 and |d| <= 1, third derivatives of a log-sum-exp at most
