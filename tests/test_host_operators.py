@@ -91,6 +91,17 @@ def test_expert_block_workspaces():
                 assert bw(T, H, F, dt) >= T * F * 4 + 2 * T * F * size + 3 * H * F * size + 2 * T * H * size + 3 * T * F * size
 
 
+def test_expert_block_plans_of_every_small_shape():
+    """The plans divide by numbers of tiles and steps: none of them is zero."""
+    for code, unit in ((binding.MOEP_BF16, 64), (binding.MOEP_F32, 4)):
+        for T in (0, 1, 2, 31, 32, 33, 63, 64, 65, 777, 10 ** 6):
+            for H in (unit, 2 * unit, 5 * unit, 64 * unit):
+                for F in (unit, 2 * unit, 9 * unit, 64 * unit):
+                    backward = binding.expert_ffn_backward_workspace(T, H, F, code)
+                    forward = [binding.expert_ffn_forward_workspace(T, H, F, code, save) for save in (False, True)]
+                    assert (backward > 0) == (T > 0) and all((n > 0) == (T > 0) for n in forward)
+
+
 @pytest.mark.parametrize("bad", [
     lambda z, i, t: pkg.moe_token_logprobs(z, i[:, 0].long()),                           # (on the host)
     lambda z, i, t: pkg.moe_token_logprobs(z[0], i[0].long()),
