@@ -341,8 +341,9 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
  *     (logits or log probabilities: a constant added to a row of them changes nothing)
  *   weights [T] fp32, may be NULL (1)
  * An alternative with ids outside [0, V) or a teacher logit of -inf is not there; an id that comes several
- * times counts as often.  A row of weight 0 is left out: its logits are not read, its loss, stats and
- * gradient are 0.  So are loss and gradient of a row without alternatives, or of nothing but -inf.
+ * times counts as often.  A row of weight 0 is left out: its logits are not read, its loss and gradient are 0,
+ * its stats -inf and 0, from which the backward call makes 0 whatever grad_loss holds for it.  Loss and gradient are
+ * 0 as well for a row without alternatives, or of nothing but -inf.
  * moe_distill_topk_backward: the gradient alone, from the stats of the forward call and the upstream
  * gradient of every loss, grad_loss [T] fp32 (a row where it is 0 is not read and gets 0).  grad may be the logits' own memory. */
 int moe_distill_topk(const void* logits, int64_t ld, const int32_t* ids, const float* teacher, int64_t T,

@@ -689,7 +689,8 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
     for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0});
   };
   if (weight == 0.f) {                                       // the row is left out: its logits are not read
-    if (MODE != GRADIENT && tid == 0) { p.loss[t] = 0.f; p.stats[2 * t] = 0.f; p.stats[2 * t + 1] = 0.f; }
+    // (stats of a row without a distribution: its loss is a constant, whatever gradient of it the backward call is given)
+    if (MODE != GRADIENT && tid == 0) { p.loss[t] = 0.f; p.stats[2 * t] = NEG_INF; p.stats[2 * t + 1] = 0.f; }
     if (MODE != LOSS) write_zeros();
     return;
   }

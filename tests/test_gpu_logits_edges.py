@@ -1,0 +1,36 @@
+"""moe_distill_topk where its arguments go to their ends, against the definition in 64 bits; bounds as in test_gpu_logits."""
+import pytest
+import torch
+
+import paper_2402_14800_amd as pkg
+from tests.test_gpu_logits import DEV, check_gradient, make_logits, make_teacher, ref_distill
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [70, 4099, 33000, 140000])
+def test_rows_left_out_of_the_loss_have_no_gradient(V, dtype):
+    """The loss of a row of weight 0 is the constant 0: whatever comes back for it, its gradient is 0, also where its logits would
+    overflow an exponential or hold NaN."""
+    T, tau = 9, 1.5
+    z = make_logits(T, V, dtype, seed=40)
+    z[2] += 300.0
+    z[5] = float("nan")
+    z[8] = -z[8].abs() - 200.0
+    ids, teacher = make_teacher(torch.nan_to_num(z), 8, seed=41)
+    weights = torch.ones(T, device=DEV)
+    out = [0, 2, 5, 8]
+    weights[out] = 0.0
+    upstream = torch.linspace(0.5, 2.0, T, device=DEV)
+    kept = [t for t in range(T) if t not in out]
+    want = ref_distill(z[kept], ids[kept], teacher[kept], tau, upstream[kept])[1]
+    for gradient in (False, True):
+        loss, stats, *_ = pkg.moe_distill_topk(z, ids, teacher, tau, weights=weights, gradient=gradient)
+        assert not bool(loss[out].any())
+        back = pkg.moe_distill_topk_backward(z, ids, teacher, stats, upstream, tau)
+        assert bool((back[out] == 0).all())
+        check_gradient(back[kept], want, upstream[kept] * tau, dtype)
+        z2 = z.clone()                                       # in the logits' own memory
+        pkg.moe_distill_topk_backward(z2, ids, teacher, stats, upstream, tau, out=z2)
+        assert torch.equal(z2, back)
