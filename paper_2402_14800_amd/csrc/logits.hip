@@ -742,11 +742,12 @@ __global__ __launch_bounds__(B) void distill_topk_kernel(DistillArgs p) {
       for (int h = 0; h < 2; ++h) {
         const int j = tid + 64 * h;
         const float q = teacher.q[j];
-        if (teacher.id[j] >= 0 && !(q == 0.f)) x += q * (teacher.log_q[j] - ((teacher.z[j] - m) / p.tau - log_s));
+        // (the logits' difference is not divided by the temperature: below 1 that overflows for the type's lowest value as a mask)
+        if (teacher.id[j] >= 0 && !(q == 0.f)) x += q * fmaf(p.tau, teacher.log_q[j] + log_s, m - teacher.z[j]);
       }
     x = sum_over_wave(x);
     if (tid == 0) {
-      p.loss[t] = p.tau * p.tau * x;
+      p.loss[t] = p.tau * x;
       p.stats[2 * t] = m;
       p.stats[2 * t + 1] = m == NEG_INF ? 0.f : log_s;
     }

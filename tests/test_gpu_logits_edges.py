@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2402_14800_amd as pkg
-from tests.test_gpu_logits import DEV, check_gradient, make_logits, make_teacher, ref_distill
+from tests.test_gpu_logits import ABS, DEV, check_gradient, make_logits, make_teacher, ref_distill
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,18 @@ def test_rows_left_out_of_the_loss_have_no_gradient(V, dtype):
         z2 = z.clone()                                       # in the logits' own memory
         pkg.moe_distill_topk_backward(z2, ids, teacher, stats, upstream, tau, out=z2)
         assert torch.equal(z2, back)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tau", [0.5, 0.7, 1.0, 1.5])
+def test_alternative_masked_by_the_lowest_value(tau, dtype):
+    """The student masks one of four equal alternatives with its type's lowest value: the loss is tau / 4 of that, a number of 32 bits."""
+    z = make_logits(3, 500, dtype, seed=42)
+    ids, _ = make_teacher(z, 4, seed=43)
+    teacher = torch.zeros((3, 4), device=DEV)
+    z[1, ids[1, 2].long()] = torch.finfo(dtype).min
+    want, rgrad = ref_distill(z, ids, teacher, tau)
+    loss, stats, grad = pkg.moe_distill_topk(z, ids, teacher, tau, gradient=True)
+    assert bool(((loss.double().cpu() - want).abs() <= ABS * want.abs() + 4 * ABS * max(1.0, tau) ** 2).all()), (loss, want)
+    check_gradient(grad, rgrad, torch.full((3,), tau), dtype)
+    check_gradient(pkg.moe_distill_topk_backward(z, ids, teacher, stats, torch.ones(3, device=DEV), tau), rgrad, torch.full((3,), tau), dtype)
