@@ -333,7 +333,9 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
 /* Distillation of a (pruned) student from the K best logits that a teacher gave for each token, as
  * moe_token_logprobs keeps them.  Of every row, q = softmax(teacher / temperature) over the row's
  * alternatives, p = softmax(logits / temperature) over all V:
- *   loss [T] fp32 (out): temperature^2 sum_j q_j (log q_j - log p_ids[j])
+ *   temperature: 2^-60 .. 2^60
+ *   loss [T] fp32 (out): temperature^2 sum_j q_j (log q_j - log p_ids[j]); the logarithms are off by about 1e-6, hence
+ *     a loss at a high temperature by about 1e-6 temperature^2
  *   stats [T,2] fp32 (out): m = max logits and log sum_i exp((logits_i - m) / temperature), for the backward call
  *   grad [T,V] dt (out, may be NULL): weights[t] times the gradient of loss[t] by the row's logits,
  *     weights[t] temperature (p - q); row t starts at t ld_grad; may be the logits' own memory (with ld_grad = ld)

@@ -875,7 +875,8 @@ int launch_distill(const DistillArgs& whole, int64_t T, moep_dtype dt, hipStream
 
 int check_teacher(const char* who, int64_t T, int K, const void* ids, const void* teacher, float tau) {
   if (K < 1 || K > MAX_K) return fail(MOEP_EINVAL, "%s: K=%d out of range [1, %d]", who, K, MAX_K);
-  if (!(tau > 0.f) || tau > 1e30f) return fail(MOEP_EINVAL, "%s: temperature %g must be positive and finite", who, (double)tau);
+  // (beyond, tau^2 or 1 / tau has no 32-bit number: the loss would be infinite or not a number)
+  if (!(tau >= 0x1p-60f && tau <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: temperature %g out of range [2^-60, 2^60]", who, (double)tau);
   if (T > 0 && (!ids || !teacher)) return fail(MOEP_EINVAL, "%s: NULL teacher ids or logits", who);
   return MOEP_OK;
 }

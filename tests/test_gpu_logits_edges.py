@@ -49,3 +49,17 @@ def test_alternative_masked_by_the_lowest_value(tau, dtype):
     assert bool(((loss.double().cpu() - want).abs() <= ABS * want.abs() + 4 * ABS * max(1.0, tau) ** 2).all()), (loss, want)
     check_gradient(grad, rgrad, torch.full((3,), tau), dtype)
     check_gradient(pkg.moe_distill_topk_backward(z, ids, teacher, stats, torch.ones(3, device=DEV), tau), rgrad, torch.full((3,), tau), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tau", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
+def test_temperatures_to_their_ends(tau, dtype):
+    """Cold, p and q pick one entry each and the loss is tau times a difference of logits; hot, both are level and it is tau^2 log(V / K)."""
+    T, V, K = 5, 1003, 8
+    z = make_logits(T, V, dtype, seed=44)
+    ids, teacher = make_teacher(z, K, seed=45)
+    want, rgrad = ref_distill(z, ids, teacher, tau)
+    loss, stats, grad = pkg.moe_distill_topk(z, ids, teacher, tau, gradient=True)
+    assert bool(((loss.double().cpu() - want).abs() <= ABS * want.abs()).all()), (loss, want)
+    check_gradient(grad, rgrad, torch.full((T,), tau), dtype)
+    check_gradient(pkg.moe_distill_topk_backward(z, ids, teacher, stats, torch.ones(T, device=DEV), tau), rgrad, torch.full((T,), tau), dtype)
