@@ -302,7 +302,7 @@ int expert_selection_stats(const float* logits, int64_t T, int E, int k, int r, 
  * Backward, from dy [T,H] (dt), the gradient of y:
  *   dx [T,H] (dt, out, may be NULL: not wanted)
  *   dW1, dW3 [F,H], dW2 [H,F] (dt, out, all three or none): overwritten, not accumulated; zero for T = 0
- * Sums are fp32; da, db and h (the gradients of the branches and the product) are rounded to dt once, as the
+ * T: up to 2^30, fp32 2^30 - 64.  Sums are fp32; da, db and h (the gradients of the branches and the product) are rounded to dt once, as the
  * GEMMs read them, and the outputs once.  All operands 16-byte aligned; none of the outputs may overlap an input.
  * Workspace: the matching queries (`keep`: whether gate_up is wanted). */
 size_t expert_ffn_forward_workspace(int64_t T, int H, int F, moep_dtype dt, int keep);

@@ -442,6 +442,8 @@ static size_t part_bytes(int64_t M, int64_t N, int ranges) { return ranges > 1 ?
 
 static int check_ffn(const char* who, int64_t T, int H, int F, moep_dtype dt) {
   if (!valid_shape(T, 1, H, F, dt, who)) return MOEP_EINVAL;
+  if (dt == MOEP_F32 && ceil_div(T, 64) > most_workgroups(256))   // (row tiles of the fp32 GEMM, workgroups of 256)
+    return fail(MOEP_EUNSUPPORTED, "%s: T=%lld is too large for fp32", who, (long long)T);
   return check_alignment(H, F, dt, who);
 }
 static int check_aligned(const char* who, std::initializer_list<const void*> pointers) {

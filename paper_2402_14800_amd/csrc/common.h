@@ -35,6 +35,8 @@ struct Timed {
 
 static inline size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Workgroups of `threads` that a grid may have along a dimension: a launch holds its threads along each in 32 bits.
+constexpr int64_t most_workgroups(int64_t threads) { return (((int64_t)1 << 32) - 1) / threads; }
 static inline size_t dtype_size(moep_dtype dt) { return dt == MOEP_BF16 ? 2 : 4; }
 
 // ---- one token's logits -------------------------------------------------------

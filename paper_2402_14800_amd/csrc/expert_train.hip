@@ -64,19 +64,31 @@ template <typename S> int64_t row_blocks(int64_t rows) { return ceil_div(rows, (
 int64_t column_blocks(int64_t columns) { return ceil_div(columns, 256); }
 
 // Several jobs in one launch: workgroups end[j - 1] .. end[j] - 1 work on job j.  (A launch of its own each costs 2 to 4 us, as much as
-// the job itself takes with a few hundred rows.)
+// the job itself takes with a few hundred rows.)  `first`: of a launch that begins further on, where one grid does not hold them all.
 template <typename J>
 struct Jobs {
   J job[MAX_JOBS];
   unsigned end[MAX_JOBS];
   int n;
+  unsigned first;
 };
 template <typename J>
 __device__ __forceinline__ int find_job(const Jobs<J>& p, unsigned* block) {
+  const unsigned b = blockIdx.x + p.first;
   int j = 0;
-  while (j + 1 < p.n && blockIdx.x >= p.end[j]) ++j;
-  *block = blockIdx.x - (j ? p.end[j - 1] : 0u);
+  while (j + 1 < p.n && b >= p.end[j]) ++j;
+  *block = b - (j ? p.end[j - 1] : 0u);
   return j;
+}
+// `launch(first, n)`: workgroups of 256 first .. first + n - 1 of `blocks`, in as many launches as the grids' limit takes.
+template <typename F>
+int in_launches(int64_t blocks, F launch) {
+  constexpr int64_t MOST = most_workgroups(256);
+  for (int64_t first = 0; first < blocks; first += MOST) {
+    launch(first, (unsigned)(blocks - first < MOST ? blocks - first : MOST));
+    MOEP_HIP(hipGetLastError());
+  }
+  return MOEP_OK;
 }
 
 struct TransposeArgs {
@@ -115,6 +127,7 @@ struct BranchArgs {
   const float* dh; const float* g; const float* u;
   int parts, F;
   int64_t T, part_stride;
+  unsigned first;                            // row block that the launch begins with
   Operand dab, da_t, db_t, h_t;
 };
 
@@ -143,7 +156,7 @@ template <bool SUMMED> constexpr int BRANCH_THREADS = SUMMED ? 64 : 256;
 template <typename S, bool SUMMED>
 __global__ __launch_bounds__(BRANCH_THREADS<SUMMED>) void branch_gradients_kernel(BranchArgs p) {
   constexpr int N = N_OF<S>, ROWS = SUMMED ? 4 : 2;
-  const Place<S, BRANCH_THREADS<SUMMED>> at(blockIdx.x, blockIdx.y);
+  const Place<S, BRANCH_THREADS<SUMMED>> at(blockIdx.x + p.first, blockIdx.y);
   if (at.c0 >= p.F || at.r0 >= p.da_t.K) return;
   u32x4 a[N], b[N], h[N], out[N];
 #pragma unroll
@@ -264,33 +277,36 @@ int launch_transposes(const TransposeJob* jobs, int n, moep_dtype dt, hipStream_
     p.end[j] = (unsigned)blocks;
   }
   Timed t("transpose", s);
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(transpose_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(transpose_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-  MOEP_HIP(hipGetLastError());
-  return MOEP_OK;
+  return in_launches(blocks, [&](int64_t first, unsigned n) {
+    p.first = (unsigned)first;
+    if (dt == MOEP_BF16) hipLaunchKernelGGL(transpose_kernel<uint16_t>, dim3(n), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(transpose_kernel<float>, dim3(n), dim3(256), 0, s, p);
+  });
 }
 
 int launch_gradients_of_branches(const float* dh, int parts, const float* g, const float* u, int64_t T, int F, moep_dtype dt, const Operand& dab,
                                  const Operand& da_t, const Operand& db_t, const Operand& h_t, hipStream_t s) {
-  BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, dab, da_t, db_t, h_t};
+  BranchArgs p = {dh, g, u, parts, F, T, T * (int64_t)F, 0, dab, da_t, db_t, h_t};
   if (!p.da_t.p) p.da_t.K = T;
   Timed t("branch_gradients", s);
-  const unsigned rows = (unsigned)(dt == MOEP_BF16 ? row_blocks<uint16_t>(p.da_t.K) : row_blocks<float>(p.da_t.K));
+  const int64_t rows = dt == MOEP_BF16 ? row_blocks<uint16_t>(p.da_t.K) : row_blocks<float>(p.da_t.K);
+  return in_launches(rows, [&](int64_t first, unsigned n) {  // (along the rows; columns are few)
+    p.first = (unsigned)first;
 #define MOEP_BRANCH(S, SUMMED)                                                                                                    \
-  hipLaunchKernelGGL((branch_gradients_kernel<S, SUMMED>), dim3(rows, (unsigned)ceil_div(F, BRANCH_THREADS<SUMMED>)), dim3(BRANCH_THREADS<SUMMED>), 0, s, p)
-  if (dt == MOEP_BF16) { if (parts > 1) MOEP_BRANCH(uint16_t, true); else MOEP_BRANCH(uint16_t, false); }
-  else if (parts > 1) MOEP_BRANCH(float, true);
-  else MOEP_BRANCH(float, false);
+  hipLaunchKernelGGL((branch_gradients_kernel<S, SUMMED>), dim3(n, (unsigned)ceil_div(F, BRANCH_THREADS<SUMMED>)), dim3(BRANCH_THREADS<SUMMED>), 0, s, p)
+    if (dt == MOEP_BF16) { if (parts > 1) MOEP_BRANCH(uint16_t, true); else MOEP_BRANCH(uint16_t, false); }
+    else if (parts > 1) MOEP_BRANCH(float, true);
+    else MOEP_BRANCH(float, false);
 #undef MOEP_BRANCH
-  MOEP_HIP(hipGetLastError());
-  return MOEP_OK;
+  });
 }
 
 int launch_silu_product(const float* g, const float* u, int64_t n, float* h, hipStream_t s) {
   Timed t("silu_product", s);
-  hipLaunchKernelGGL(silu_product_kernel, dim3((unsigned)ceil_div(n / 4, 256)), dim3(256), 0, s, (const f32x4*)g, (const f32x4*)u, n / 4, (f32x4*)h);
-  MOEP_HIP(hipGetLastError());
-  return MOEP_OK;
+  return in_launches(ceil_div(n / 4, 256), [&](int64_t first, unsigned blocks) {
+    const int64_t i = first * 256;
+    hipLaunchKernelGGL(silu_product_kernel, dim3(blocks), dim3(256), 0, s, (const f32x4*)g + i, (const f32x4*)u + i, n / 4 - i, (f32x4*)h + i);
+  });
 }
 
 int launch_sums(const SumJob* jobs, int n, moep_dtype dt, hipStream_t s) {
@@ -306,10 +322,11 @@ int launch_sums(const SumJob* jobs, int n, moep_dtype dt, hipStream_t s) {
     p.end[j] = (unsigned)blocks;
   }
   Timed t("sum_parts", s);
-  if (dt == MOEP_BF16) hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(sum_parts_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-  MOEP_HIP(hipGetLastError());
-  return MOEP_OK;
+  return in_launches(blocks, [&](int64_t first, unsigned n) {
+    p.first = (unsigned)first;
+    if (dt == MOEP_BF16) hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, dim3(n), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(sum_parts_kernel<float>, dim3(n), dim3(256), 0, s, p);
+  });
 }
 
 int launch_clear(void* p, size_t bytes, hipStream_t s) {

@@ -248,7 +248,7 @@ int launch_gemm_f32(const GemmArgs& g, hipStream_t s, const char* name) {
   const int64_t tiles = (g.segments ? routed_row_tiles(g.M, g.busy_experts, tm) : ceil_div(g.M, tm)) * n_tiles(tb) * g.experts;
   const int ahead = (f.by_register && tiles > 512) || g.rows_unknown ? 1 : f32_slabs_ahead(tiles, 2, tm == 64 ? 3 : 4);
   const int64_t row_tiles = ceil_div(g.M, tm) + g.segments;
-  if (row_tiles > 2147483647LL || n_tiles(tb) > GRID_Y_MAX) return fail(MOEP_EUNSUPPORTED, "%s: too many tiles", name);
+  if (row_tiles > most_workgroups(THREADS) || n_tiles(tb) > GRID_Y_MAX) return fail(MOEP_EUNSUPPORTED, "%s: too many tiles", name);
   dim3 grid((unsigned)row_tiles, (unsigned)n_tiles(tb), (unsigned)g.experts);
   f.columns_first = f32_columns_first(g.segments > 0, row_tiles);
   if (f.columns_first) grid = dim3((unsigned)n_tiles(tb), (unsigned)row_tiles, 1);

@@ -839,8 +839,9 @@ int check_rows(const char* who, int64_t T, int64_t V, moep_dtype dt, const void*
   return MOEP_OK;
 }
 
-// Rows of a launch: a grid has fewer than 2^32 threads.
-constexpr int64_t LAUNCH_ROWS = (int64_t)1 << 22;
+// Rows of a launch, of up to 1024 threads each.
+constexpr int64_t LAUNCH_ROWS = (int64_t)1 << 21;
+static_assert(LAUNCH_ROWS <= most_workgroups(1024), "one workgroup a row");
 
 template <int MODE>
 int launch_distill(const DistillArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
