@@ -393,14 +393,6 @@ int moe_expert_outputs_packed(const void* x, const void* Wgate, const void* pack
 }
 
 // ------------------------------------------------------------------ expert_ffn
-// Ranges of K for a product of `M` x `N` outputs (tile_plan.h): bf16 tiles of 256 x 256 on as many compute units, ranges of at least
-// 512; fp32 tiles of 32 x 64, four to a compute unit, ranges of at least 128.
-static int ranges_of(int64_t M, int64_t N, int64_t K, moep_dtype dt, bool any) {
-  if (dt == MOEP_BF16) return (int)k_ranges(ceil_div(M, 256) * ceil_div(N, 256), 256, ceil_div(K, 64), 8, any);
-  if (!any && K % 32) return 1;
-  return (int)k_ranges(ceil_div(M, 32) * ceil_div(N, 64), 1024, ceil_div(K, 32), 4, any);
-}
-
 // C [M,N] (dt) = A B^T, in `ranges` ranges of K through `part` (ranges [M,N] fp32 matrices; only for several ranges).  bf16: both
 // operands packed, or B row-major.
 struct Product {
@@ -438,7 +430,6 @@ static int multiply(const Product& q, moep_dtype dt, void* C, float* part, SumJo
   g.M = q.M; g.N = q.N; g.K = q.K; g.epilogue = EPI_STORE;
   return launch_gemm_bf16_packed(g, s, name);
 }
-static size_t part_bytes(int64_t M, int64_t N, int ranges) { return ranges > 1 ? align256((size_t)ranges * M * N * 4) : 0; }
 
 static int check_ffn(const char* who, int64_t T, int H, int F, moep_dtype dt) {
   if (!valid_shape(T, 1, H, F, dt, who)) return MOEP_EINVAL;
@@ -510,50 +501,9 @@ int expert_ffn_forward(const void* x, const void* W1, const void* W3, const void
   return launch_sums(sum, n_sums, dt, s);
 }
 
-// The backward call's workspace.  `t_parts` ranges along the tokens for dW2, half as many (where even) for dW1 and dW3, which have
-// twice the tiles; K of the transposed operands is T padded to whole ranges.
-struct FfnBackwardPlan {
-  bool together;                                  // the last three products in one launch (tile_plan.h)
-  int dh_parts, dx_parts, t_parts, t_parts13;
-  int64_t Tp, rows13;                             // rows13: rows of da^T | db^T as one operand
-  size_t dy, w2t, dh, dab, w13t, x_t, dy_t, dadb_t, h_t, dx_part, w13_part, w2_part, total;
-};
-static int plan_ffn_backward(int64_t T, int H, int F, moep_dtype dt, FfnBackwardPlan* p) {
-  p->dh_parts = ranges_of(T, F, H, dt, false);
-  p->dx_parts = ranges_of(T, H, 2 * (int64_t)F, dt, false);
-  p->t_parts = ranges_of(H, F, T, dt, true);
-  p->t_parts13 = p->t_parts % 2 ? p->t_parts : p->t_parts / 2;
-  const BackwardCut cut = cut_backward(T, H, F);
-  p->together = dt == MOEP_BF16 && cut.together;
-  if (p->together) {
-    p->dx_parts = (int)cut.dx_ranges;
-    p->t_parts = p->t_parts13 = (int)cut.t_ranges;
-  }
-  const int64_t unit = (dt == MOEP_BF16 ? 64 : p->t_parts > 1 ? 32 : 4) * (int64_t)p->t_parts;
-  p->Tp = ceil_div(T, unit) * unit;
-  if (p->Tp >= (int64_t)1 << 31) return fail(MOEP_EUNSUPPORTED, "expert_ffn_backward: T=%lld is too large", (long long)T);
-  p->rows13 = dt == MOEP_BF16 ? 2 * ceil_div(F, 256) * 256 : 2 * (int64_t)F;
-  size_t at = 0;
-  auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
-  p->dy = take(dt == MOEP_BF16 ? operand_bytes(T, H, dt) : 0);
-  p->w2t = take(operand_bytes(F, H, dt));
-  p->dh = take((size_t)p->dh_parts * T * F * 4);
-  p->dab = take(operand_bytes(T, 2 * (int64_t)F, dt));
-  p->w13t = take(operand_bytes(H, 2 * (int64_t)F, dt));
-  p->x_t = take(operand_bytes(H, p->Tp, dt));
-  p->dy_t = take(operand_bytes(H, p->Tp, dt));
-  p->dadb_t = take(operand_bytes(p->rows13, p->Tp, dt));
-  p->h_t = take(operand_bytes(F, p->Tp, dt));
-  p->dx_part = take(part_bytes(T, H, p->dx_parts));
-  p->w13_part = take(part_bytes(p->rows13, H, p->t_parts13));
-  p->w2_part = take(part_bytes(H, F, p->t_parts));
-  p->total = at;
-  return MOEP_OK;
-}
-
 size_t expert_ffn_backward_workspace(int64_t T, int H, int F, moep_dtype dt) {
   FfnBackwardPlan p;
-  if (check_ffn("expert_ffn_backward_workspace", T, H, F, dt) || T == 0 || plan_ffn_backward(T, H, F, dt, &p)) return 0;
+  if (check_ffn("expert_ffn_backward_workspace", T, H, F, dt) || T == 0 || !plan_ffn_backward(T, H, F, dt, &p)) return 0;
   return p.total;
 }
 
@@ -577,7 +527,7 @@ int expert_ffn_backward(const void* dy, const void* x, const void* W1, const voi
   if (!dx && !weights) return MOEP_OK;
   if (!dy || !gate_up || (weights && !x)) return fail(MOEP_EINVAL, "%s: NULL dy, x or gate_up", who);
   FfnBackwardPlan p;
-  if (int st = plan_ffn_backward(T, H, F, dt, &p)) return st;
+  if (!plan_ffn_backward(T, H, F, dt, &p)) return fail(MOEP_EUNSUPPORTED, "%s: T=%lld is too large", who, (long long)T);
   if (int st = check_ws(ws, ws_bytes, p.total, who)) return st;
   char* const at = (char*)ws;
   const bool bf16 = dt == MOEP_BF16;

@@ -7,6 +7,7 @@
 #include <stddef.h>
 
 #include "enum_plan.h"
+#include "ffn_plan.h"
 #include "moeprune.h"
 #include "skip_plan.h"
 #include "tile_plan.h"
@@ -326,7 +327,6 @@ struct Operand {
   int64_t rows = 0, K = 0;
   bool weight = false;
 };
-size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt);
 // X [R, C] transposed into columns k0 .. of `out` (rows C, K at least k0 + R; columns k0 + R .. k_end - 1 are cleared); `straight`
 // (bf16, p may be NULL): X itself as an operand of R rows as well.  Several of them in one launch.
 struct TransposeJob {

@@ -260,10 +260,6 @@ __global__ __launch_bounds__(256) void clear_kernel(u32x4* p, int64_t n) {
 
 }  // namespace
 
-size_t operand_bytes(int64_t rows, int64_t K, moep_dtype dt) {
-  return dt == MOEP_BF16 ? (size_t)ceil_div(rows, 256) * 256 * (size_t)K * 2 : (size_t)rows * (size_t)K * 4;
-}
-
 int launch_transposes(const TransposeJob* jobs, int n, moep_dtype dt, hipStream_t s) {
   if (n < 1 || n > MAX_JOBS) return fail(MOEP_EINVAL, "transposes: %d jobs", n);
   Jobs<TransposeArgs> p = {};
