@@ -63,3 +63,33 @@ def test_temperatures_to_their_ends(tau, dtype):
     assert bool(((loss.double().cpu() - want).abs() <= ABS * want.abs()).all()), (loss, want)
     check_gradient(grad, rgrad, torch.full((T,), tau), dtype)
     check_gradient(pkg.moe_distill_topk_backward(z, ids, teacher, stats, torch.ones(T, device=DEV), tau), rgrad, torch.full((T,), tau), dtype)
+
+
+def test_rows_that_are_not_rows_of_logits_are_refused():
+    """On the GPU, where nothing but their strides is wrong."""
+    V = 64
+    z = make_logits(V, V, torch.float32, seed=46)
+    ids, teacher = make_teacher(z, 3, seed=47)
+    tokens = ids[:, 0].long().contiguous()
+    stats, ones = torch.zeros((V, 2), device=DEV), torch.ones(V, device=DEV)
+    overlapping = torch.zeros(2 * V, device=DEV).as_strided((V, V), (1, 1))
+    repeated = z[:1].expand(V, V)
+    for bad in (z.t(), torch.zeros((V, 2 * V), device=DEV)[:, ::2], overlapping, repeated):
+        assert bad.shape == (V, V) and bad.is_cuda
+        for call in (lambda: pkg.moe_token_logprobs(bad, tokens), lambda: pkg.moe_distill_topk(bad, ids, teacher),
+                     lambda: pkg.moe_distill_topk_backward(bad, ids, teacher, stats, ones),
+                     lambda: pkg.moe_distill_topk(z, ids, teacher, gradient=True, out=bad),
+                     lambda: pkg.moe_distill_topk_backward(z, ids, teacher, stats, ones, out=bad)):
+            with pytest.raises(ValueError, match="rows of logits must be contiguous"):
+                call()
+    for bad in (ids.t().contiguous().t(), ids.long(), ids.cpu(), ids[:-1], ids[:, :2]):
+        with pytest.raises(ValueError):
+            pkg.moe_distill_topk(z, bad, teacher)
+    for bad in (tokens.cpu(), tokens.int(), tokens[:-1], torch.cat([tokens, tokens])[::2]):
+        with pytest.raises(ValueError, match="tokens must be"):
+            pkg.moe_token_logprobs(z, bad)
+    for bad in (ones[:1].expand(V), ones.double(), ones[:-1]):
+        with pytest.raises(ValueError, match="grad_loss must be"):
+            pkg.moe_distill_topk_backward(z, ids, teacher, stats, bad)
+        with pytest.raises(ValueError, match="weights must be"):
+            pkg.moe_distill_topk(z, ids, teacher, weights=bad)
