@@ -338,7 +338,9 @@ int moe_token_logprobs(const void* logits, int64_t ld, const int64_t* tokens, in
  *     a loss at a high temperature by about 1e-6 temperature^2
  *   stats [T,2] fp32 (out): m = max logits and log sum_i exp((logits_i - m) / temperature), for the backward call
  *   grad [T,V] dt (out, may be NULL): weights[t] times the gradient of loss[t] by the row's logits,
- *     weights[t] temperature (p - q); row t starts at t ld_grad; may be the logits' own memory (with ld_grad = ld)
+ *     weights[t] temperature (p - q); row t starts at t ld_grad; may be the logits' own memory (with ld_grad = ld).
+ *     Rows that start like the logits' rows within 16 bytes are stored by 16 bytes, others element by element: bf16, rows of
+ *     32001 logits of which 32000 are used, 4096 of them, 122 us with ld_grad = 32001, 225 with 32000
  *   logits: as in moe_token_logprobs;  ids [T,K] int32, teacher [T,K] fp32, 1 <= K <= 128
  *     (logits or log probabilities: a constant added to a row of them changes nothing)
  *   weights [T] fp32, may be NULL (1)

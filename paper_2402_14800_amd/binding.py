@@ -638,7 +638,8 @@ def _alternatives(ids, teacher, T: int, index: int) -> int:
 def moe_distill_topk(logits, ids, teacher, temperature: float = 1.0, weights=None, gradient: bool = False, out=None):
     """loss [T] and stats [T,2] (fp32) of the student's logits [T,V] against the teacher's alternatives, ids [T,K] int32 and
     teacher [T,K] fp32; with `gradient` also the gradient of (weights * loss).sum() by the logits, in the same pass, into
-    `out` if given (which may be `logits` itself)."""
+    `out` if given (which may be `logits` itself), else into rows of V elements.  Of logits that are views into longer rows of
+    which not all start alike within 16 bytes the gradient is written fastest into an `out` of the same layout."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
     dev = logits.device

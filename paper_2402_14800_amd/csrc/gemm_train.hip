@@ -5,7 +5,7 @@
 // launch (tile_plan.h).
 //
 // Bound by the matrix rate under the power cap where the product is large, 8192 rows of H 4096, F 14336: gate/up with the branches 1410 to
-// 1460 us (1.32 to 1.36 PFLOP/s; about 225 us of it are the 0.94 GB of branches in its epilogue), dh 661 to 705 us (1.36 to 1.46, its
+// 1475 us (1.30 to 1.36 PFLOP/s; about 225 us of it are the 0.94 GB of branches in its epilogue), dh 655 to 705 us (1.36 to 1.47, its
 // result in fp32); dx 1165 to 1210 (1.6), dW1 and dW3 1200 to 1240 (1.6), dW2 672 to 705 (1.4) have the plain epilogue.  777 rows of H 1024, F 3584: 24, 17 and 47
 // us (dx and the three gradients in one launch, 0.61), one round of tiles with its fill and drain.
 #include "gemm_packed_kernel.h"

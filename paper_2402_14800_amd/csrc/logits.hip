@@ -3,16 +3,16 @@
 //
 // With m = max_i z_i, s = sum_i exp((z_i - m) / tau):  log p_i = (z_i - m) / tau - log s, and (tau = 1) the entropy is
 // log s - sum_i exp(z_i - m) (z_i - m) / s.  With q the softmax of the teacher's K logits over tau, the loss of a row is
-// tau^2 sum_j q_j (log q_j - log p_id(j)) and its gradient tau (p - q).
+// tau^2 sum_j q_j (log q_j - log p_id(j)), added up as tau sum_j q_j (tau (log q_j + log s) + m - z_id(j)), and its gradient tau (p - q).
 //
 // Bound by the one read of the logits (and the one write of the gradient); the lanes are close behind: an element of two
 // bytes costs about ten lane operations, four of them the exponential.  A workgroup takes a row; each thread keeps its own
 // running maximum and sums (a rescale per 16 chunks), so the row is read without a barrier and joined once at its end.  Up to
 // 16 chunks of 16 bytes per thread stay in registers, so a row of up to 32768 bf16 logits on 256 threads is read from memory
 // once also where it is used again (the gradient, the search for the best); a longer one is walked tile by tile.
-// Time and bytes read and written: 1999 rows of 32000 bf16, K = 1 32.0 us (4.0 TB/s; the launch's beginning and its last workgroups cost 6 us
-// of it), 2048 of 131072, K = 64 115 us (4.7); loss and gradient of 4096 of 32000, K = 64 102 us (5.2, the rate of a copy), of 2048 of
-// 131072, K = 100 227 us (4.7); one row of 32000, K = 20 9 us, the workgroup's own way through it.
+// Time and bytes read and written: 1999 rows of 32000 bf16, K = 1 32.0 us (4.0 TB/s: 1280 workgroups fit the chip, so these are 1.6 rounds of
+// them), 2048 of 131072, K = 64 114 us (4.7); loss and gradient of 4096 of 32000, K = 64 103 us (5.1, the rate of a copy), of 2048 of
+// 131072, K = 100 227 to 234 us (4.6 to 4.7); one row of 32000, K = 20 9 us, the workgroup's own way through it.
 // (Workgroups that stay and ask for their next row while they end the present one were slower everywhere, 1.1 to 1.7 times: loads and
 // stores return in order, so a row's first chunk waited for the stores before it. More workgroups than fit do the same without.)
 #include <type_traits>
@@ -313,7 +313,9 @@ struct SearchSpace {
 
 // The exact threshold where the shortcut below collects too many elements (equal logits by the thousand): the K-th largest key, eight
 // bits at a time, then by the same means the index up to which elements of just that key are taken, lowest first.  Nine short walks
-// of the row.
+// of the row: 2048 rows of 32000 equal bf16 logits, K = 64 988 us for 43, one of them 279 for 14.  Short rows come here with ordinary logits
+// too, where K comes near the threads that the threshold is taken from, whole wavefronts with a chunk each: 2100 rows of 1000, K = 20 10.5 us,
+// 33 21.5, 64 118, 128 83.
 template <typename S, int B>
 __device__ void select_exactly(const S* z, int V, int K, SearchSpace<B>* q) {
   const int tid = threadIdx.x;
@@ -657,6 +659,8 @@ __device__ __forceinline__ bool weigh(const DistillArgs& p, const Alternatives& 
   return !(m == NEG_INF);
 }
 
+// `aligned`: whether the gradient's row starts like the logits' within 16 bytes.  Else all of a chunk's elements are stored by themselves:
+// loss and gradient of 4096 rows of 32000 bf16 in rows of 32001, the gradient in rows of 32000, 225 us for 122, the gradient alone 215 for 122.
 template <typename S>
 __device__ __forceinline__ void store_chunk(const Row<S>& row, S* out, bool aligned, int c, u32x4 v) {
   const int i0 = c * Row<S>::N - row.lead;
