@@ -358,6 +358,92 @@ int moe_distill_topk_backward(const void* logits, int64_t ld, const int32_t* ids
                               moep_dtype dt, float temperature, void* grad, int64_t ld_grad,
                               void* hip_stream);
 
+/* ---- moe_dispatch_rows, moe_combine_rows ----------------------------------------- */
+/* A token's row on its way to the experts and back: what runs the experts' blocks of a layer (expert_ffn_forward and
+ * expert_ffn_backward) on the rows routed to each.  Slot j of token t, 0 <= j < k, goes to expert experts[t,j]:
+ *   x [T,H] (dt), experts [T,k] int32, 1 <= k <= 16, T k <= 2^30, e.g. top2_out or topk_out of the forward calls
+ *   used [T] int32, may be NULL (k): slots j >= used[t] are not used, e.g. n_used of moe_forward_skip_topk
+ *   rows [T*k,H] dt (out): x[t] for every slot that is used, sorted by expert, then token, then j.  Rows offsets[E] .. T*k - 1 are
+ *     left as they were
+ *   slot_of [T,k] int32 (out): the row of rows that holds slot j of token t; -1 where the slot is not used
+ *   offsets [E+1] int32 (out): rows offsets[e] .. offsets[e+1] - 1 are expert e's
+ * A slot whose expert lies outside [0, E) is not used; a token that names an expert twice has two rows there.  T = 0: all offsets 0.
+ * Workspace: moe_dispatch_rows_workspace (0 up to 8192 slots: one launch, else two).
+ * moe_dispatch_rows_backward: dx [T,H] = sum over the used slots of drows [R,H], in the order of j.
+ * moe_combine_rows: out [T,H] = sum over the used slots of weights[t,j] y[slot_of[t,j]], y [R,H] (the experts' output rows); a token
+ *   without a used slot gives zeros.  weights [T,k] fp32, may be NULL (1).
+ * moe_combine_rows_backward, from dout [T,H], the gradient of out:
+ *   dy [R,H] dt (out): weights[t,j] dout[t] in row slot_of[t,j]; rows that no slot names are left as they were.  May be y's memory
+ *   dweights [T,k] fp32 (out, may be NULL: not wanted, y is not read): <dout[t], y[slot_of[t,j]]>, 0 for a slot that is not used
+ * In these three R is the number of rows (T*k for those of moe_dispatch_rows) and a slot outside [0, R) is not used; in the last one no
+ * two slots may name one row.  What a weight multiplies is not read where its slot is not used; a used slot's weight 0 multiplies.
+ * Products and sums are fp32, rounded to dt once.  None of the outputs may overlap an input (but dy with y). */
+size_t moe_dispatch_rows_workspace(int64_t T, int k, int E);
+int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used, int64_t T, int k, int E, int H,
+                      moep_dtype dt, void* rows, int32_t* slot_of, int32_t* offsets, void* ws, size_t ws_bytes,
+                      void* hip_stream);
+int moe_dispatch_rows_backward(const void* drows, const int32_t* slot_of, int64_t T, int k, int H, int64_t R,
+                               moep_dtype dt, void* dx, void* hip_stream);
+int moe_combine_rows(const void* y, const int32_t* slot_of, const float* weights, int64_t T, int k, int H, int64_t R,
+                     moep_dtype dt, void* out, void* hip_stream);
+int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* slot_of, const float* weights, int64_t T,
+                              int k, int H, int64_t R, moep_dtype dt, void* dy, float* dweights, void* hip_stream);
+
+/* ---- moe_policy_loss --------------------------------------------------------- */
+/* The clipped policy loss of sampled tokens with a KL term, for reinforcement on the pruned model's own answers.  Of every row, with
+ * lp = log softmax(logits / temperature) at the row's token, r = exp(lp - old_logprob) and A its advantage:
+ *   loss = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(d) - d - 1),  d = ref_logprob - lp
+ *   logits: as in moe_token_logprobs;  tokens [T] int64
+ *   old_logprob, advantages [T] fp32;  ref_logprob [T] fp32, may be NULL where kl is 0 (and is not read there)
+ *   clip_low 0 .. 1, clip_high and kl 0 .. 2^60, temperature 2^-60 .. 2^60
+ *   loss, logprob [T] fp32 (out): the loss and lp
+ *   stats [T,3] fp32 (out): m = max logits, log sum_i exp((logits_i - m) / temperature), and the loss's derivative by lp, for the
+ *     backward call
+ *   grad [T,V] dt (out, may be NULL): weights[t] times the gradient of loss[t] by the row's logits; rows and memory as in
+ *     moe_distill_topk (may be the logits' own, with ld_grad = ld)
+ *   weights [T] fp32, may be NULL (1)
+ * A row with a negative token (a prompt's, or padding) or of weight 0 is left out: its logits, and with a negative token what else
+ * belongs to it, count for nothing; loss, logprob and gradient are 0, stats -inf, 0, 0.  A token of V or more: NaN.  An advantage of 0 leaves
+ * the KL term alone, however large r.  Where the clip holds, the first term's derivative is 0 (at r = the bound itself it does not hold).
+ * A loss beyond 32 bits is infinite (a KL term with a token of probability 0, say, or a negative advantage with an r that is), and its
+ * row's gradient 0.
+ * moe_policy_loss_backward: the gradient alone, from the stats and the upstream gradient of every loss, grad_loss [T] fp32 (a row where
+ * it, or the derivative, is 0 is not read and gets 0).  grad may be the logits' own memory. */
+int moe_policy_loss(const void* logits, int64_t ld, const int64_t* tokens, const float* old_logprob,
+                    const float* advantages, const float* ref_logprob, int64_t T, int64_t V, moep_dtype dt,
+                    float clip_low, float clip_high, float kl, float temperature, const float* weights, float* loss,
+                    float* logprob, float* stats, void* grad, int64_t ld_grad, void* hip_stream);
+int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const float* stats,
+                             const float* grad_loss, int64_t T, int64_t V, moep_dtype dt, float temperature, void* grad,
+                             int64_t ld_grad, void* hip_stream);
+
+/* ---- moe_preference_loss ----------------------------------------------------- */
+/* The loss of paired answers, one preferred to the other, on the log ratios of the model to a reference.  Answer a is the rows
+ * offsets[a] .. offsets[a+1] - 1 of the logits; pair i is answers i (chosen) and pairs + i (rejected).  Of an answer,
+ * D = sum over its rows that have a token of (log softmax(logits) at the token - ref_logprob), average = 1: divided by how many those are.
+ *   loss[i] = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h),  h = beta (D_chosen - D_rejected)
+ *   logits: as in moe_token_logprobs;  tokens [T] int64 (negative: none, e.g. a prompt's; V or more: NaN)
+ *   offsets [2*pairs+1] int64, DEVICE, ascending within [0, T];  an answer may be empty (D = 0).  Offsets in another order give
+ *     unspecified results, within the arrays
+ *   ref_logprob [T] fp32;  0 < beta <= 2^60;  0 <= smoothing < 1;  0 <= pairs <= 2^22
+ *   loss [pairs], rewards [2,pairs] fp32 (out): rewards are beta D of the chosen, then of the rejected answers
+ *   logprob [T] fp32 (out), stats [T,3] fp32 (out): as in moe_policy_loss, the derivative being that of the row's pair; 0 and -inf, 0, 0
+ *     for rows without a token or outside all answers, whose logits are not read
+ *   grad [T,V] dt (out, may be NULL): weights[i] times the gradient of loss[i] by the logits of its answers' rows; memory as in
+ *     moe_distill_topk.  0 for their rows without a token; rows outside all answers are left as they were
+ *   weights [pairs] fp32, may be NULL (1)
+ * Sums over an answer are fp64.  The logits are read twice where the gradient is wanted: a pair's derivative needs both whole answers.
+ * A token of probability 0 makes its pair's loss what the formula gives: infinite, 0, or (both answers) NaN, and the derivative with it.
+ * moe_preference_loss_backward: the gradient alone, from the stats and grad_loss [pairs] fp32 (rows where it is 0 are not read and get
+ * 0).  grad may be the logits' own memory in both. */
+int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
+                        const float* ref_logprob, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, float beta,
+                        float smoothing, int average, const float* weights, float* loss, float* rewards,
+                        float* logprob, float* stats, void* grad, int64_t ld_grad, void* hip_stream);
+int moe_preference_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
+                                 const float* stats, const float* grad_loss, int64_t T, int64_t V, int64_t pairs,
+                                 moep_dtype dt, void* grad, int64_t ld_grad, void* hip_stream);
+
 /* ---- per-kernel timing (for benchmarks) ------------------------------------ */
 /* While enabled, every kernel launch is bracketed by HIP events on its stream.
  * moep_timing_collect waits for the recorded events, adds them up per kernel and

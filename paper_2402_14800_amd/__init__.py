@@ -14,6 +14,8 @@ _BINDING_NAMES = (
     "moe_expert_outputs_ranked", "prune_enumerate_ranked",
     "expert_ffn_forward", "expert_ffn_backward",
     "moe_token_logprobs", "moe_distill_topk", "moe_distill_topk_backward",
+    "moe_policy_loss", "moe_policy_loss_backward", "moe_preference_loss", "moe_preference_loss_backward",
+    "moe_dispatch_rows", "moe_dispatch_rows_backward", "moe_combine_rows", "moe_combine_rows_backward",
     "num_subsets", "subset_unrank", "subset_rank", "library_path", "MoepError",
     "kernel_timing_enable", "kernel_timing_collect", "kernel_timing_reset", "kernel_timing_records", "mfma_ceiling",
 )

@@ -34,6 +34,8 @@ EXPORTS = (
     "moe_expert_outputs_ranked_workspace", "moe_expert_outputs_ranked", "prune_enumerate_ranked",
     "moe_token_logprobs", "moe_distill_topk", "moe_distill_topk_backward",
     "expert_ffn_forward_workspace", "expert_ffn_forward", "expert_ffn_backward_workspace", "expert_ffn_backward",
+    "moe_dispatch_rows_workspace", "moe_dispatch_rows", "moe_dispatch_rows_backward", "moe_combine_rows", "moe_combine_rows_backward",
+    "moe_policy_loss", "moe_policy_loss_backward", "moe_preference_loss", "moe_preference_loss_backward",
     "moep_timing_enable", "moep_timing_collect", "moep_timing_records", "moep_mfma_ceiling",
 )
 
@@ -148,6 +150,27 @@ def _load() -> ctypes.CDLL:
     lib.moe_distill_topk_backward.restype = c_int
     lib.moe_distill_topk_backward.argtypes = [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
                                               c_int, c_int, c_float, c_void_p, c_int64, c_void_p]
+    lib.moe_dispatch_rows_workspace.restype = c_size_t
+    lib.moe_dispatch_rows_workspace.argtypes = [c_int64, c_int, c_int]
+    lib.moe_dispatch_rows.restype = c_int
+    lib.moe_dispatch_rows.argtypes = [c_void_p] * 3 + [c_int64, c_int, c_int, c_int, c_int] + [c_void_p] * 4 + [c_size_t, c_void_p]
+    lib.moe_dispatch_rows_backward.restype = c_int
+    lib.moe_dispatch_rows_backward.argtypes = [c_void_p] * 2 + [c_int64, c_int, c_int, c_int64, c_int, c_void_p, c_void_p]
+    lib.moe_combine_rows.restype = c_int
+    lib.moe_combine_rows.argtypes = [c_void_p] * 3 + [c_int64, c_int, c_int, c_int64, c_int, c_void_p, c_void_p]
+    lib.moe_combine_rows_backward.restype = c_int
+    lib.moe_combine_rows_backward.argtypes = [c_void_p] * 4 + [c_int64, c_int, c_int, c_int64, c_int] + [c_void_p] * 3
+    lib.moe_policy_loss.restype = c_int
+    lib.moe_policy_loss.argtypes = [c_void_p, c_int64] + [c_void_p] * 4 + [c_int64, c_int64, c_int] + [c_float] * 4 + \
+        [c_void_p] * 5 + [c_int64, c_void_p]
+    lib.moe_policy_loss_backward.restype = c_int
+    lib.moe_policy_loss_backward.argtypes = [c_void_p, c_int64] + [c_void_p] * 3 + [c_int64, c_int64, c_int, c_float, c_void_p, c_int64, c_void_p]
+    lib.moe_preference_loss.restype = c_int
+    lib.moe_preference_loss.argtypes = [c_void_p, c_int64] + [c_void_p] * 3 + [c_int64, c_int64, c_int64, c_int, c_float, c_float, c_int] + \
+        [c_void_p] * 6 + [c_int64, c_void_p]
+    lib.moe_preference_loss_backward.restype = c_int
+    lib.moe_preference_loss_backward.argtypes = [c_void_p, c_int64] + [c_void_p] * 4 + [c_int64, c_int64, c_int64, c_int, c_void_p, c_int64,
+                                                                                         c_void_p]
     lib.moep_timing_enable.restype = c_int
     lib.moep_timing_enable.argtypes = [c_int]
     lib.moep_timing_collect.restype = c_int
@@ -576,6 +599,98 @@ def expert_ffn_backward(dy, x, W1, W3, W2, gate_up, input_gradient: bool = True,
     return dx, dW1, dW3, dW2
 
 
+# ---------------------------------------------------------------- rows to the experts and back
+# (sizes as plain numbers: torch.empty takes 0.4 us longer for a tuple, and these calls allocate several small tensors)
+_empty = torch.empty
+
+# Kernels go to the current device; where the tensors lie on another one, that is made current for the call.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call_on(dev: torch.device, call, *args) -> None:
+    """call(*args, stream) with `dev` the current device, and its status checked."""
+    if _current_device() == dev.index:
+        _check(call(*args, _raw_stream(dev.index)))
+    else:
+        with torch.cuda.device(dev):
+            _check(call(*args, _raw_stream(dev.index)))
+
+
+def _slot_rows(rows, slot_of, what: str):
+    """T, k, H, R and the type code of rows [R,H] named by slot_of [T,k]."""
+    if rows.dim() != 2 or slot_of.dim() != 2 or slot_of.dtype != torch.int32:
+        raise ValueError(f"{what}: rows must be [R, H] and slot_of [T, k] in int32")
+    return slot_of.shape[0], slot_of.shape[1], rows.shape[1], rows.shape[0], _dtype_code(rows)
+
+
+def _slot_weights(weights, slot_of, what: str):
+    if weights is not None and (weights.shape != slot_of.shape or weights.dtype != torch.float32):
+        raise ValueError(f"{what}: weights must be [T, k] in float32, as slot_of is")
+
+
+def moe_dispatch_rows_workspace(T: int, k: int, E: int) -> int:
+    return int(_lib.moe_dispatch_rows_workspace(T, k, E))
+
+
+def moe_dispatch_rows(x, experts, num_experts: int, used=None, rows=None, workspace=None):
+    """rows [T*k,H], slot_of [T,k] int32 and offsets [num_experts+1] int32: every token's row of x [T,H] copied to the experts [T,k] int32
+    that it goes to, sorted by expert.  `used` [T] int32: how many of a token's slots are used (None: all).  `rows`, if given, is written
+    in place; what lies behind the last used row stays as it was (without it: is not initialised)."""
+    if x.dim() != 2 or experts.dim() != 2 or experts.shape[0] != x.shape[0] or experts.dtype != torch.int32:
+        raise ValueError("moe_dispatch_rows: x must be [T, H] and experts [T, k] in int32")
+    T, H = x.shape
+    k = experts.shape[1]
+    dt = _dtype_code(x)
+    if used is not None and (used.shape != (T,) or used.dtype != torch.int32):
+        raise ValueError("moe_dispatch_rows: used must be [T] in int32")
+    if rows is not None and (rows.shape != (T * k, H) or rows.dtype != x.dtype):
+        raise ValueError("moe_dispatch_rows: rows must be [T * k, H], of x's type")
+    dev = _dev(*(t for t in (x, experts, used, rows) if t is not None))
+    if rows is None:
+        rows = _empty(T * k, H, dtype=x.dtype, device=dev)
+    slot_of = _empty(T, k, dtype=torch.int32, device=dev)
+    offsets = _empty(max(num_experts, 0) + 1, dtype=torch.int32, device=dev)
+    need = _lib.moe_dispatch_rows_workspace(T, k, num_experts)
+    ws = _workspace(need, dev, workspace) if need or workspace is not None else None
+    _call_on(dev, _lib.moe_dispatch_rows, _ptr(x), _ptr(experts), _ptr(used), T, k, num_experts, H, dt, _ptr(rows), _ptr(slot_of),
+             _ptr(offsets), _ptr(ws), ws.numel() if ws is not None else 0)
+    return rows, slot_of, offsets
+
+
+def moe_dispatch_rows_backward(drows, slot_of):
+    """dx [T,H]: the gradients of a token's rows added up, from drows [R,H] and moe_dispatch_rows's slot_of [T,k]."""
+    T, k, H, R, dt = _slot_rows(drows, slot_of, "moe_dispatch_rows_backward")
+    dev = _dev(drows, slot_of)
+    dx = _empty(T, H, dtype=drows.dtype, device=dev)
+    _call_on(dev, _lib.moe_dispatch_rows_backward, _ptr(drows), _ptr(slot_of), T, k, H, R, dt, _ptr(dx))
+    return dx
+
+
+def moe_combine_rows(y, slot_of, weights=None):
+    """out [T,H]: the experts' output rows y [R,H] weighted (weights [T,k] fp32, None: 1) and added up by token."""
+    T, k, H, R, dt = _slot_rows(y, slot_of, "moe_combine_rows")
+    _slot_weights(weights, slot_of, "moe_combine_rows")
+    dev = _dev(y, slot_of) if weights is None else _dev(y, slot_of, weights)
+    out = _empty(T, H, dtype=y.dtype, device=dev)
+    _call_on(dev, _lib.moe_combine_rows, _ptr(y), _ptr(slot_of), _ptr(weights), T, k, H, R, dt, _ptr(out))
+    return out
+
+
+def moe_combine_rows_backward(dout, y, slot_of, weights=None, weight_gradient: bool = True, dy=None):
+    """dy [R,H] and dweights [T,k] fp32 (None without `weight_gradient`) from dout [T,H].  `dy`, if given, is written in place (it may be y);
+    rows that no slot names stay as they were (without it: are not initialised)."""
+    T, k, H, R, dt = _slot_rows(y, slot_of, "moe_combine_rows_backward")
+    _slot_weights(weights, slot_of, "moe_combine_rows_backward")
+    if dout.shape != (T, H) or dout.dtype != y.dtype or (dy is not None and (dy.shape != y.shape or dy.dtype != y.dtype)):
+        raise ValueError("moe_combine_rows_backward: dout must be [T, H] and dy like y, of y's type")
+    dev = _dev(*(t for t in (y, dout, slot_of, weights, dy) if t is not None))
+    if dy is None:
+        dy = _empty(R, H, dtype=y.dtype, device=dev)
+    dweights = _empty(T, k, dtype=torch.float32, device=dev) if weight_gradient else None
+    _call_on(dev, _lib.moe_combine_rows_backward, _ptr(dout), _ptr(y), _ptr(slot_of), _ptr(weights), T, k, H, R, dt, _ptr(dy), _ptr(dweights))
+    return dy, dweights
+
+
 # ---------------------------------------------------------------- logits
 def _logit_rows(logits):
     """T, V and the distance between rows of a 2-D tensor whose rows may lie further apart than they are long."""
@@ -596,10 +711,6 @@ def _beside(t, shape, dtype, index: int, what: str):
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
     if t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous and on the logits' GPU")
-
-
-# (sizes as plain numbers: torch.empty takes 0.4 us longer for a tuple, and these calls allocate several small tensors)
-_empty = torch.empty
 
 
 def moe_token_logprobs(logits, tokens, top: int = 0):
@@ -665,6 +776,90 @@ def moe_distill_topk_backward(logits, ids, teacher, stats, grad_loss, temperatur
     _check(_lib.moe_distill_topk_backward(logits.data_ptr(), ld, ids.data_ptr(), teacher.data_ptr(), stats.data_ptr(),
                                           grad_loss.data_ptr(), T, V, K, dt, temperature, grad.data_ptr(), ld_grad,
                                           _raw_stream(dev.index)))
+    return grad
+
+
+# ---------------------------------------------------------------- losses on given answers
+def moe_policy_loss(logits, tokens, old_logprob, advantages, ref_logprob=None, clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0,
+                    temperature: float = 1.0, weights=None, gradient: bool = False, out=None):
+    """loss [T], logprob [T] and stats [T,3] (fp32) of sampled tokens [T] int64 (negative: left out) under logits [T,V], from the log
+    probabilities with which they were sampled, their advantages and, with `kl`, a reference's log probabilities (all [T] fp32); with
+    `gradient` also the gradient of (weights * loss).sum() by the logits, in the same pass, into `out` if given (which may be `logits`)."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    dev = logits.device
+    _beside(tokens, (T,), torch.int64, dev.index, "tokens")
+    _beside(old_logprob, (T,), torch.float32, dev.index, "old_logprob")
+    _beside(advantages, (T,), torch.float32, dev.index, "advantages")
+    if ref_logprob is not None:
+        _beside(ref_logprob, (T,), torch.float32, dev.index, "ref_logprob")
+    if weights is not None:
+        _beside(weights, (T,), torch.float32, dev.index, "weights")
+    loss, logprob = _empty(T, dtype=torch.float32, device=dev), _empty(T, dtype=torch.float32, device=dev)
+    stats = _empty(T, 3, dtype=torch.float32, device=dev)
+    grad, ld_grad = _gradient_rows(logits, out, T, V) if gradient else (None, 0)
+    _call_on(dev, _lib.moe_policy_loss, logits.data_ptr(), ld, tokens.data_ptr(), old_logprob.data_ptr(), advantages.data_ptr(), _ptr(ref_logprob),
+             T, V, dt, clip_low, clip_high, kl, temperature, _ptr(weights), loss.data_ptr(), logprob.data_ptr(), stats.data_ptr(), _ptr(grad), ld_grad)
+    return (loss, logprob, stats, grad) if gradient else (loss, logprob, stats)
+
+
+def moe_policy_loss_backward(logits, tokens, stats, grad_loss, temperature: float = 1.0, out=None):
+    """The gradient [T,V] by the logits, from moe_policy_loss's stats and the upstream gradient [T] fp32 of its loss."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    dev = logits.device
+    _beside(tokens, (T,), torch.int64, dev.index, "tokens")
+    _beside(stats, (T, 3), torch.float32, dev.index, "stats")
+    _beside(grad_loss, (T,), torch.float32, dev.index, "grad_loss")
+    grad, ld_grad = _gradient_rows(logits, out, T, V)
+    _call_on(dev, _lib.moe_policy_loss_backward, logits.data_ptr(), ld, tokens.data_ptr(), stats.data_ptr(), grad_loss.data_ptr(), T, V, dt,
+             temperature, grad.data_ptr(), ld_grad)
+    return grad
+
+
+def _pairs(offsets, index: int) -> int:
+    if offsets.dim() != 1 or offsets.shape[0] % 2 == 0:
+        raise ValueError("offsets must be [2 * pairs + 1]")
+    _beside(offsets, offsets.shape, torch.int64, index, "offsets")
+    return offsets.shape[0] // 2
+
+
+def moe_preference_loss(logits, tokens, offsets, ref_logprob, beta: float = 0.1, smoothing: float = 0.0, average: bool = False, weights=None,
+                        gradient: bool = False, out=None):
+    """loss [P], rewards [2,P], logprob [T] and stats [T,3] (fp32) of P pairs of answers: answer a is rows offsets[a] .. offsets[a+1] - 1 of
+    logits [T,V], offsets [2 P + 1] int64; pair i is answers i (chosen) and P + i (rejected); tokens [T] int64 (negative: none), ref_logprob
+    [T] fp32.  With `gradient` also the gradient of (weights * loss).sum(), weights [P], by the logits, into `out` if given (which may be
+    `logits`); its rows outside all answers stay as they were (without `out`: are not initialised)."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    dev = logits.device
+    P = _pairs(offsets, dev.index)
+    _beside(tokens, (T,), torch.int64, dev.index, "tokens")
+    _beside(ref_logprob, (T,), torch.float32, dev.index, "ref_logprob")
+    if weights is not None:
+        _beside(weights, (P,), torch.float32, dev.index, "weights")
+    loss, rewards = _empty(P, dtype=torch.float32, device=dev), _empty(2, P, dtype=torch.float32, device=dev)
+    logprob, stats = _empty(T, dtype=torch.float32, device=dev), _empty(T, 3, dtype=torch.float32, device=dev)
+    grad, ld_grad = _gradient_rows(logits, out, T, V) if gradient else (None, 0)
+    _call_on(dev, _lib.moe_preference_loss, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), ref_logprob.data_ptr(), T, V, P, dt, beta,
+             smoothing, 1 if average else 0, _ptr(weights), loss.data_ptr(), rewards.data_ptr(), logprob.data_ptr(), stats.data_ptr(), _ptr(grad),
+             ld_grad)
+    return (loss, rewards, logprob, stats, grad) if gradient else (loss, rewards, logprob, stats)
+
+
+def moe_preference_loss_backward(logits, tokens, offsets, stats, grad_loss, out=None):
+    """The gradient [T,V] by the logits, from moe_preference_loss's stats and the upstream gradient [P] fp32 of its loss.  Rows outside all
+    answers stay as they were in `out` (without it: are not initialised)."""
+    T, V, ld = _logit_rows(logits)
+    dt = _dtype_code(logits)
+    dev = logits.device
+    P = _pairs(offsets, dev.index)
+    _beside(tokens, (T,), torch.int64, dev.index, "tokens")
+    _beside(stats, (T, 3), torch.float32, dev.index, "stats")
+    _beside(grad_loss, (P,), torch.float32, dev.index, "grad_loss")
+    grad, ld_grad = _gradient_rows(logits, out, T, V)
+    _call_on(dev, _lib.moe_preference_loss_backward, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), stats.data_ptr(),
+             grad_loss.data_ptr(), T, V, P, dt, grad.data_ptr(), ld_grad)
     return grad
 
 

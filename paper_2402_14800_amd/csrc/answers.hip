@@ -1,0 +1,410 @@
+// Losses on given answers, and their gradients by the logits: the clipped policy loss of sampled tokens (moe_policy_loss) and the loss of
+// paired answers (moe_preference_loss).
+//
+// Of a row z with its token y, lp = (z_y - m) / tau - log s (m, s as in logits.hip), and both losses reach the logits through lp alone:
+// with c the loss's derivative by lp, the gradient is c (onehot_y - p) / tau.
+//   policy:      r = exp(lp - old), loss = -min(r A, clip(r) A) + kl (exp(e) - e - 1) with e = ref - lp,
+//                c = -r A (0 where the clip holds) - kl (exp(e) - 1)
+//   preference:  D = sum over an answer's tokens of lp - ref (or their mean), h = beta (D_chosen - D_rejected),
+//                loss = -(1 - ls) log sigmoid(h) - ls log sigmoid(-h), c = +-(ls - sigmoid(-h)) beta (over the number of tokens)
+// Bound by the read of the logits and the write of the gradient.  The policy loss knows c as soon as its row is summed, so the row stays in
+// registers and is read once; a pair's c needs all rows of both answers, so the gradient reads the logits again, last rows first.
+#include "logits_rows.h"
+
+namespace moep {
+namespace {
+
+enum AnswerMode { LOSS = 0, LOSS_AND_GRADIENT = 1, GRADIENT = 2 };
+
+struct AnswerArgs {
+  const void* logits; int64_t ld, T; int V;
+  const int64_t* tokens;                     // [T]; negative: none
+  float tau;
+  // policy, LOSS*
+  const float* old; const float* advantages; const float* ref;
+  float low, high, kl;                       // 1 - clip, 1 + clip
+  const float* up;                           // LOSS*: the rows' weights (optional); GRADIENT: the upstream gradient of each row's or pair's loss (optional)
+  // preference
+  const int64_t* offsets;                    // [2 pairs + 1]; NULL: policy
+  int64_t pairs, first;                      // `first`: the launch's first row
+  float* loss; float* logprob;
+  float* stats;                              // [T, 3]: m, log s, c (GRADIENT reads them)
+  void* grad; int64_t ld_grad;
+};
+
+// exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, 1e-9 of the sum.)
+__device__ __forceinline__ float exp_beyond_line(float x) {
+  if (fabsf(x) < 0.5f) {
+    float s = 1.f / 362880.f;
+    s = fmaf(s, x, 1.f / 40320.f);
+    s = fmaf(s, x, 1.f / 5040.f);
+    s = fmaf(s, x, 1.f / 720.f);
+    s = fmaf(s, x, 1.f / 120.f);
+    s = fmaf(s, x, 1.f / 24.f);
+    s = fmaf(s, x, 1.f / 6.f);
+    s = fmaf(s, x, 0.5f);
+    return s * x * x;
+  }
+  const float e = expm1f(x);
+  return e == -NEG_INF ? e : e - x;                          // (x may be infinite itself)
+}
+
+struct Term { float loss, slope; };
+__device__ __forceinline__ Term policy_term(const AnswerArgs& p, float lp, float old, float A, float ref) {
+  Term t = {0.f, 0.f};
+  if (!(A == 0.f)) {                                         // (nothing to gain either way, also where r is infinite)
+    const float r = expf(lp - old);
+    // the ratio has gone as far as it may the way the advantage asks for
+    const bool far = A > 0.f ? r > p.high : r < p.low;
+    t.loss = far ? -(A > 0.f ? p.high : p.low) * A : -r * A;
+    t.slope = far ? 0.f : -r * A;
+  }
+  if (p.ref) {
+    const float e = ref - lp;
+    t.loss = fmaf(p.kl, exp_beyond_line(e), t.loss);
+    t.slope = fmaf(-p.kl, expm1f(e), t.slope);
+  }
+  if (fabsf(t.loss) == -NEG_INF) t.slope = 0.f;              // (an exponential beyond 32 bits: no gradient that could be followed)
+  return t;
+}
+
+// The answer that row t belongs to: how many of the n ascending offsets are <= t, less one.  64 of them are looked at at once, by every
+// wavefront for itself: one round trip up to 63, two up to 4095.  (Offsets in any other order end as well, and within [-1, n).)
+// In 32 bits (n < 2^24): of a 64-bit comparison that picked a bound and ended the loop as well, the compiler kept the loop's end alone.
+__device__ __forceinline__ int answer_of(const int64_t* offsets, int n, int64_t t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;                                        // those in front of lo are <= t, those from hi on are not
+  while (lo < hi) {
+    const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step - 1;
+    const int k = __popcll(__ballot(at < hi && offsets[at] <= t));
+    hi = min(hi, lo + (k + 1) * step - 1);
+    lo = min(lo + k * step, hi);
+  }
+  return lo - 1;
+}
+
+// HELD: the row fits the workgroup's registers (LOSS_AND_GRADIENT, the one mode that uses a row twice).
+template <typename S, int B, int MODE, bool HELD>
+__global__ __launch_bounds__(B) void answers_kernel(AnswerArgs p) {
+  constexpr int N = Elements<S>::N;
+  __shared__ float shared[3 * (B / 64)];
+  int tid = threadIdx.x;
+  // (a pair's gradient: the rows that the loss read last are the ones that the caches still hold)
+  const int64_t t = MODE == GRADIENT && p.offsets ? p.T - 1 - blockIdx.x : blockIdx.x;
+  const Row<S> row(p.logits, p.ld, p.V, t, p.T);
+  const int tiles = HELD ? 1 : (row.chunks + B * NC - 1) / (B * NC);
+  S* const out = MODE == LOSS ? nullptr : (S*)p.grad + t * p.ld_grad;
+  const bool aligned = (((uintptr_t)out ^ (uintptr_t)row.at) & 15) == 0;
+  auto write_zeros = [&]() {
+    for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0});
+  };
+  const int64_t y = p.tokens[t];
+  const float c = uniform(LOG2E / p.tau);
+  float m, scale, factor, shift = 0.f;                       // the gradient is scale [i = y] - factor exp2((z - m) c + shift)
+  u32x4 v[NC];
+  if (MODE != GRADIENT) {
+    bool left_out = y < 0;
+    if (p.offsets) left_out = left_out || p.first + t < p.offsets[0] || p.first + t >= p.offsets[2 * p.pairs];
+    const float weight = !p.offsets && p.up ? uniform(p.up[t]) : 1.f;
+    if (left_out || weight == 0.f) {                         // its logits are not read
+      if (tid == 0) {
+        if (!p.offsets) p.loss[t] = 0.f;
+        p.logprob[t] = 0.f;
+        p.stats[3 * t] = NEG_INF; p.stats[3 * t + 1] = 0.f; p.stats[3 * t + 2] = 0.f;
+      }
+      if (MODE == LOSS_AND_GRADIENT) write_zeros();
+      return;
+    }
+    float zy = y < p.V ? Elements<S>::load(row.at + y) : __builtin_nanf("");
+    float old = 0.f, A = 0.f, ref = 0.f;
+    if (!p.offsets) {
+      old = p.old[t]; A = p.advantages[t];
+      if (p.ref) ref = p.ref[t];
+    }
+    Stats all = {NEG_INF, 0.f, 0.f};
+    for (int i = 0; i < tiles; ++i) {
+      tid = thread_again(tid);
+      request_tile<S, B>(row, i, tid, v);
+      cut_ends<S, B>(row, i, tid, v);
+      add_tile<S, B, false>(v, row.chunks - i * (B * NC), all, c);
+    }
+    zy = uniform(zy);                                        // (here before anybody writes: grad may be the logits' own memory)
+    all = join_wave<B, false>(all, c, shared);
+    __syncthreads();
+    all = join_all<B, false>(all, c, shared);
+    m = uniform(all.m);
+    const float log_s = uniform(logf(all.s));
+    float lp = m == NEG_INF ? NEG_INF : (zy - m) / p.tau - log_s;
+    if (!(y < p.V)) lp = __builtin_nanf("");
+    Term term = {0.f, 0.f};
+    if (!p.offsets) term = policy_term(p, lp, old, A, ref);
+    if (tid == 0) {
+      if (!p.offsets) p.loss[t] = term.loss;
+      p.logprob[t] = lp;
+      p.stats[3 * t] = m; p.stats[3 * t + 1] = m == NEG_INF ? 0.f : log_s; p.stats[3 * t + 2] = term.slope;
+    }
+    if (MODE == LOSS) return;
+    scale = uniform(term.slope * weight / p.tau);
+    factor = uniform(scale / all.s);
+    if (term.slope == 0.f) {
+      write_zeros();
+      return;
+    }
+  } else {
+    const float slope = uniform(p.stats[3 * t + 2]);
+    m = uniform(p.stats[3 * t]);
+    shift = uniform(-p.stats[3 * t + 1] * LOG2E);
+    float up = 1.f;
+    if (p.offsets) {
+      const int pairs = (int)p.pairs, a = answer_of(p.offsets, 2 * pairs + 1, p.first + t);
+      if (a < 0 || a >= 2 * pairs) return;                   // a row of no answer: as it was
+      if (p.up) up = uniform(p.up[a < pairs ? a : a - pairs]);
+    } else if (p.up) {
+      up = uniform(p.up[t]);
+    }
+    if (slope == 0.f || up == 0.f || m == NEG_INF || y < 0) { // (its logits are not read; nothing but -inf has no distribution)
+      write_zeros();
+      return;
+    }
+    scale = uniform(slope * up / p.tau);
+    factor = scale;
+  }
+  const int at_y = y < p.V ? (int)((y + row.lead) / N) : -1, of_y = y < p.V ? (int)((y + row.lead) % N) : 0;
+  for (int i = 0; i < tiles; ++i) {
+    tid = thread_again(tid);
+    if (!HELD || MODE == GRADIENT) {
+      request_tile<S, B>(row, i, tid, v);
+      cut_ends<S, B>(row, i, tid, v);
+    } else {
+      use_again(v);
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const int at = i * (B * NC) + n * B + tid;
+      if (at < row.chunks) {
+        float x[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float d = Elements<S>::get(v[n], j) - m;
+          x[j] = -factor * exp2_fast(MODE == GRADIENT ? fmaf(d, c, shift) : d * c);
+        }
+        if (at == at_y)
+#pragma unroll
+          for (int j = 0; j < N; ++j) x[j] += j == of_y ? scale : 0.f;
+        store_chunk(row, out, aligned, at, Elements<S>::pack(x));
+      }
+    }
+  }
+}
+
+// A pair: both answers' sums of lp - ref in 64 bits, the loss, the rewards, and c of every row of theirs.
+struct PairArgs {
+  const int64_t* tokens; const int64_t* offsets; const float* ref; const float* logprob;
+  int64_t T, pairs, first;                   // `first`: of the launch
+  float beta, smoothing;
+  int average;
+  float* loss; float* rewards; float* stats;
+};
+constexpr int PAIR_THREADS = 256;
+
+__global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
+  __shared__ double sums[2][PAIR_THREADS / 64];
+  __shared__ int64_t given[2][PAIR_THREADS / 64];
+  const int tid = threadIdx.x;
+  const int64_t pair = p.first + blockIdx.x;
+  int64_t r0[2], r1[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const int64_t a = side ? p.pairs + pair : pair;
+    r0[side] = max((int64_t)0, min(p.T, p.offsets[a]));
+    r1[side] = max((int64_t)0, min(p.T, p.offsets[a + 1]));
+  }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    double x = 0;
+    int64_t n = 0;
+    for (int64_t t = r0[side] + tid; t < r1[side]; t += PAIR_THREADS)
+      if (p.tokens[t] >= 0) {
+        x += (double)p.logprob[t] - (double)p.ref[t];
+        ++n;
+      }
+    for (int d = 32; d > 0; d >>= 1) {
+      x += __shfl_xor(x, d);
+      n += __shfl_xor(n, d);
+    }
+    if ((tid & 63) == 0) { sums[side][tid >> 6] = x; given[side][tid >> 6] = n; }
+  }
+  __syncthreads();
+  double reward[2], by[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const double x = (sums[side][0] + sums[side][1]) + (sums[side][2] + sums[side][3]);
+    const int64_t n = given[side][0] + given[side][1] + given[side][2] + given[side][3];
+    by[side] = (double)p.beta / (double)(p.average && n > 0 ? n : 1);
+    reward[side] = by[side] * x;
+  }
+  const double h = reward[0] - reward[1], ls = (double)p.smoothing;
+  // -log sigmoid(h) = max(-h, 0) + log(1 + exp(-|h|)), and the other one is h more
+  const double away = log1p(exp(-fabs(h)));
+  const double loss = (1 - ls) * (fmax(-h, 0.0) + away) + (ls > 0 ? ls * (fmax(h, 0.0) + away) : 0.0);
+  const double by_h = ls - 1 / (1 + exp(h));
+  if (tid == 0) {
+    p.loss[pair] = (float)(h == h ? loss : h);
+    p.rewards[pair] = (float)reward[0];
+    p.rewards[p.pairs + pair] = (float)reward[1];
+  }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const float c = (float)((side ? -by_h : by_h) * by[side]);
+    for (int64_t t = r0[side] + tid; t < r1[side]; t += PAIR_THREADS) p.stats[3 * t + 2] = p.tokens[t] >= 0 ? c : 0.f;
+  }
+}
+
+template <int MODE>
+int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
+  const int64_t chunks = most_chunks(whole.logits, whole.ld, whole.V, dt);
+  const int threads = MODE == LOSS ? threads_to_read(T, chunks) : threads_to_hold(T, chunks);
+  Timed timed(name, s);
+  const int64_t launches = ceil_div(T, LAUNCH_ROWS);
+  for (int64_t i = 0; i < launches; ++i) {
+    const int64_t t = (MODE == GRADIENT && whole.offsets ? launches - 1 - i : i) * LAUNCH_ROWS;
+    AnswerArgs p = whole;
+    p.T = T - t < LAUNCH_ROWS ? T - t : LAUNCH_ROWS;
+    p.first = t;
+    const int64_t size = (int64_t)dtype_size(dt);
+    p.logits = (const char*)whole.logits + t * whole.ld * size;
+    p.tokens += t;
+    if (p.old) p.old += t;
+    if (p.advantages) p.advantages += t;
+    if (p.ref) p.ref += t;
+    if (p.up && !p.offsets) p.up += t;
+    if (p.loss && !p.offsets) p.loss += t;
+    if (p.logprob) p.logprob += t;
+    p.stats += 3 * t;
+    if (p.grad) p.grad = (char*)whole.grad + t * whole.ld_grad * size;
+    auto with = [&](auto b, auto held) {
+      constexpr int B = decltype(b)::value;
+      constexpr bool HELD = decltype(held)::value && MODE == LOSS_AND_GRADIENT;
+      if (dt == MOEP_BF16) hipLaunchKernelGGL((answers_kernel<uint16_t, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
+      else hipLaunchKernelGGL((answers_kernel<float, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
+    };
+    if constexpr (MODE == LOSS) {
+      if (threads == 64) with(std::integral_constant<int, 64>{}, std::false_type{});
+      else if (threads == 256) with(std::integral_constant<int, 256>{}, std::false_type{});
+      else with(std::integral_constant<int, 512>{}, std::false_type{});
+    } else {
+      constexpr auto most = std::integral_constant<int, 1024>{};
+      if (!threads) with(most, std::false_type{});
+      else if (threads == 1024) with(most, std::true_type{});
+      else with_threads(threads, [&](auto b) { with(b, std::true_type{}); });
+    }
+    MOEP_HIP(hipGetLastError());
+  }
+  return MOEP_OK;
+}
+
+int check_temperature(const char* who, float tau) {
+  // (as for distillation: beyond, 1 / tau or what it multiplies has no 32-bit number)
+  if (!(tau >= 0x1p-60f && tau <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: temperature %g out of range [2^-60, 2^60]", who, (double)tau);
+  return MOEP_OK;
+}
+int check_scalars(const char* who, std::initializer_list<const void*> of4, std::initializer_list<const void*> of8) {
+  for (const void* q : of4)
+    if ((uintptr_t)q & 3) return fail(MOEP_EUNSUPPORTED, "%s: fp32 arrays must be 4-byte aligned", who);
+  for (const void* q : of8)
+    if ((uintptr_t)q & 7) return fail(MOEP_EUNSUPPORTED, "%s: tokens and offsets must be 8-byte aligned", who);
+  return MOEP_OK;
+}
+
+}  // namespace
+}  // namespace moep
+
+using namespace moep;
+
+extern "C" {
+
+int moe_policy_loss(const void* logits, int64_t ld, const int64_t* tokens, const float* old_logprob, const float* advantages,
+                    const float* ref_logprob, int64_t T, int64_t V, moep_dtype dt, float clip_low, float clip_high, float kl, float temperature,
+                    const float* weights, float* loss, float* logprob, float* stats, void* grad, int64_t ld_grad, void* hip_stream) {
+  const char* who = "moe_policy_loss";
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (int st = check_temperature(who, temperature)) return st;
+  if (!(clip_low >= 0.f && clip_low <= 1.f)) return fail(MOEP_EINVAL, "%s: clip_low %g out of range [0, 1]", who, (double)clip_low);
+  if (!(clip_high >= 0.f && clip_high <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: clip_high %g out of range [0, 2^60]", who, (double)clip_high);
+  if (!(kl >= 0.f && kl <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: kl %g out of range [0, 2^60]", who, (double)kl);
+  if (grad)
+    if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (T == 0) return MOEP_OK;
+  if (!logits || !tokens || !old_logprob || !advantages || !loss || !logprob || !stats)
+    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, old_logprob, advantages, loss, logprob or stats", who);
+  if (kl > 0.f && !ref_logprob) return fail(MOEP_EINVAL, "%s: the KL term needs ref_logprob", who);
+  if (int st = check_scalars(who, {old_logprob, advantages, ref_logprob, weights, loss, logprob, stats}, {tokens})) return st;
+  const AnswerArgs p = {logits, ld, T, (int)V, tokens, temperature, old_logprob, advantages, kl > 0.f ? ref_logprob : nullptr, 1.f - clip_low,
+                        1.f + clip_high, kl, weights, nullptr, 0, 0, loss, logprob, stats, grad, ld_grad};
+  return grad ? launch_answers<LOSS_AND_GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "policy_loss_gradient")
+              : launch_answers<LOSS>(p, T, dt, (hipStream_t)hip_stream, "policy_loss");
+}
+
+int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const float* stats, const float* grad_loss, int64_t T,
+                             int64_t V, moep_dtype dt, float temperature, void* grad, int64_t ld_grad, void* hip_stream) {
+  const char* who = "moe_policy_loss_backward";
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (int st = check_temperature(who, temperature)) return st;
+  if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (T == 0) return MOEP_OK;
+  if (!logits || !tokens || !stats || !grad_loss || !grad) return fail(MOEP_EINVAL, "%s: NULL logits, tokens, stats, grad_loss or grad", who);
+  if (int st = check_scalars(who, {stats, grad_loss}, {tokens})) return st;
+  const AnswerArgs p = {logits, ld, T, (int)V, tokens, temperature, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, grad_loss, nullptr, 0, 0,
+                        nullptr, nullptr, (float*)stats, grad, ld_grad};
+  return launch_answers<GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "policy_gradient");
+}
+
+int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* ref_logprob, int64_t T,
+                        int64_t V, int64_t pairs, moep_dtype dt, float beta, float smoothing, int average, const float* weights, float* loss,
+                        float* rewards, float* logprob, float* stats, void* grad, int64_t ld_grad, void* hip_stream) {
+  const char* who = "moe_preference_loss";
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
+  if (!(beta > 0.f && beta <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: beta %g out of range (0, 2^60]", who, (double)beta);
+  if (!(smoothing >= 0.f && smoothing < 1.f)) return fail(MOEP_EINVAL, "%s: smoothing %g out of range [0, 1)", who, (double)smoothing);
+  if (average != 0 && average != 1) return fail(MOEP_EINVAL, "%s: average=%d is neither 0 nor 1", who, average);
+  if (grad)
+    if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (!offsets) return fail(MOEP_EINVAL, "%s: NULL offsets", who);
+  if (pairs > 0 && (!loss || !rewards)) return fail(MOEP_EINVAL, "%s: NULL loss or rewards", who);
+  if (T > 0 && (!logits || !tokens || !ref_logprob || !logprob || !stats))
+    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, ref_logprob, logprob or stats", who);
+  if (int st = check_scalars(who, {ref_logprob, weights, loss, rewards, logprob, stats}, {tokens, offsets})) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, nullptr, offsets, pairs, 0,
+                  nullptr, logprob, stats, nullptr, 0};
+  if (T > 0)
+    if (int st = launch_answers<LOSS>(p, T, dt, s, "answer_logprobs")) return st;
+  if (pairs > 0) {
+    Timed timed("pairs", s);
+    const PairArgs q = {tokens, offsets, ref_logprob, logprob, T, pairs, 0, beta, smoothing, average, loss, rewards, stats};
+    hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)pairs), dim3(PAIR_THREADS), 0, s, q);
+    MOEP_HIP(hipGetLastError());
+  }
+  if (!grad || T == 0 || pairs == 0) return MOEP_OK;
+  p.up = weights; p.grad = grad; p.ld_grad = ld_grad;
+  return launch_answers<GRADIENT>(p, T, dt, s, "preference_gradient");
+}
+
+int moe_preference_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* stats,
+                                 const float* grad_loss, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, void* grad, int64_t ld_grad,
+                                 void* hip_stream) {
+  const char* who = "moe_preference_loss_backward";
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
+  if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (T == 0 || pairs == 0) return MOEP_OK;
+  if (!logits || !tokens || !offsets || !stats || !grad_loss || !grad)
+    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, offsets, stats, grad_loss or grad", who);
+  if (int st = check_scalars(who, {stats, grad_loss}, {tokens, offsets})) return st;
+  const AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, grad_loss, offsets, pairs, 0,
+                        nullptr, nullptr, (float*)stats, grad, ld_grad};
+  return launch_answers<GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "preference_gradient");
+}
+
+}  // extern "C"

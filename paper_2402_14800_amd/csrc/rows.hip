@@ -1,0 +1,510 @@
+// A token's row on its way to the experts and back (moe_dispatch_rows, moe_combine_rows, and their gradients).
+//
+// Slot (t, j) of a token that uses it gets a number slot(t, j), counted by expert, within an expert by token, within a token by j:
+//   dispatch: rows[slot(t, j)] = x[t]             gradient: dx[t] = sum_j drows[slot(t, j)]
+//   combine:  out[t] = sum_j w[t, j] y[slot(t, j)]   gradients: dy[slot(t, j)] = w[t, j] dout[t],  dw[t, j] = <dout[t], y[slot(t, j)]>
+// All of it is bound by memory: a token's row is read once and written k times, or the other way round.  The numbers come from counting
+// alone (integers: the same whatever the order), so a workgroup works out those of its own tokens from how many ids lie before them.
+#include <type_traits>
+
+#include "common.h"
+
+namespace moep {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;   // one 16-byte chunk
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int MAX_E = 32, MAX_K = 16;
+
+// ---- dispatch --------------------------------------------------------------------------------------
+struct DispatchArgs {
+  const char* x;
+  const int32_t* experts;                    // [T, k]
+  const int32_t* used;                       // [T], may be NULL: all k
+  int64_t T;
+  int k, E, chunks;                          // chunks of 16 bytes to a row
+  int per;                                   // tokens of a workgroup
+  int32_t* counts;                           // [pieces, E] ids of each expert in pieces of `piece` tokens; NULL: not counted ahead
+  int64_t piece;
+  int pieces;
+  char* rows;
+  int32_t* slot_of;                          // [T, k]
+  int32_t* offsets;                          // [E + 1]
+};
+
+// The expert of slot i = t k + j, -1 if the slot is not used.
+__device__ __forceinline__ int expert_at(const DispatchArgs& p, unsigned i) {
+  const int e = p.experts[i];
+  bool there = (unsigned)e < (unsigned)p.E;
+  if (p.used) {
+    const unsigned t = i / (unsigned)p.k;
+    there = there && (int)(i - t * (unsigned)p.k) < p.used[t];
+  }
+  return there ? e : -1;
+}
+
+// Counts in LDS, eight copies so that the lanes of a wavefront seldom meet at one.
+constexpr int COPIES = 8;
+struct Counts { int n[COPIES][MAX_E + 1]; };
+__device__ __forceinline__ void clear(Counts* c) {
+  for (int i = threadIdx.x; i < COPIES * (MAX_E + 1); i += THREADS) (&c->n[0][0])[i] = 0;
+}
+__device__ __forceinline__ int total(const Counts& c, int e) {
+  int n = 0;
+#pragma unroll
+  for (int q = 0; q < COPIES; ++q) n += c.n[q][e];
+  return n;
+}
+// Adds the ids of slots i0 .. i1 - 1, eight of a thread's in flight.
+__device__ __forceinline__ void count(const DispatchArgs& p, unsigned i0, unsigned i1, Counts* c) {
+  int* const mine = c->n[threadIdx.x & (COPIES - 1)];
+  for (unsigned i = i0 + threadIdx.x; i < i1; i += 8 * THREADS) {
+    int e[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) e[q] = i + q * THREADS < i1 ? expert_at(p, i + q * THREADS) : -1;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (e[q] >= 0) atomicAdd(&mine[e[q]], 1);
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
+  __shared__ Counts c;
+  clear(&c);
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
+  count(p, (unsigned)(t0 * p.k), (unsigned)(t1 * p.k), &c);
+  __syncthreads();
+  if ((int)threadIdx.x < p.E) p.counts[(int64_t)blockIdx.x * p.E + threadIdx.x] = total(c, threadIdx.x);
+}
+
+// Chunks of a row that a wavefront's lanes bring at once, a multiple of 64 of them.
+constexpr int COPY = 4;
+
+__global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p) {
+  __shared__ Counts before, rest;
+  __shared__ int next[MAX_E];                // the number of the next row of each expert
+  __shared__ int of_wave[WAVES][MAX_E];
+  __shared__ int slots[THREADS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t first = (int64_t)blockIdx.x * p.per, last = min(p.T, first + p.per);
+  clear(&before);
+  clear(&rest);
+  __syncthreads();
+  if (p.counts) {
+    const int64_t mine = first / p.piece;    // (a workgroup's tokens lie in one piece)
+    for (int i = tid; i < p.pieces * p.E; i += THREADS) {
+      const int n = p.counts[i], c = i / p.E, e = i - c * p.E;
+      if (n) atomicAdd(&(c < mine ? before : rest).n[tid & (COPIES - 1)][e], n);
+    }
+    // (of the piece's own ids those in front of the workgroup's belong to `before`, and are counted in `rest` as well: taken off below)
+    __shared__ Counts twice;
+    clear(&twice);
+    __syncthreads();
+    count(p, (unsigned)(mine * p.piece * p.k), (unsigned)(first * p.k), &twice);
+    __syncthreads();
+    if (tid < p.E) {
+      const int n = total(twice, tid);
+      before.n[0][tid] += n;
+      rest.n[0][tid] -= n;
+    }
+  } else {
+    count(p, 0, (unsigned)(first * p.k), &before);
+    count(p, (unsigned)(first * p.k), (unsigned)(p.T * p.k), &rest);
+  }
+  __syncthreads();
+  if (tid < 64) {                            // rows of the experts in front, and of this one in front of the workgroup's
+    const int b = tid < p.E ? total(before, tid) : 0, n = tid < p.E ? b + total(rest, tid) : 0;
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < MAX_E; d <<= 1) {
+      const int from = __shfl_up(upto, d);
+      if (lane >= d) upto += from;
+    }
+    if (tid < MAX_E) next[tid] = upto - n + b;
+    if (blockIdx.x == 0 && tid < p.E) {
+      p.offsets[tid + 1] = upto;
+      if (tid == 0) p.offsets[0] = 0;
+    }
+  }
+  const int batch = THREADS / p.k;           // tokens whose slots are worked out at once, one to a thread
+  for (int64_t t0 = first; t0 < last; t0 += batch) {
+    const int tokens = (int)min((int64_t)batch, last - t0), n = tokens * p.k;
+    for (int i = tid; i < WAVES * MAX_E; i += THREADS) (&of_wave[0][0])[i] = 0;
+    __syncthreads();                         // (`next` is there too)
+    const int e = tid < n ? expert_at(p, (unsigned)(t0 * p.k) + tid) : -1;
+    int rank = 0;                            // among the wavefront's slots of the same expert
+    for (unsigned long long left = __ballot(e >= 0); left;) {
+      const int of = __builtin_amdgcn_readlane(e, __ffsll((long long)left) - 1);
+      const unsigned long long same = __ballot(e == of);
+      if (e == of) {
+        rank = __builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0u));
+        of_wave[wave][e] = __popcll(same);
+      }
+      left &= ~same;
+    }
+    __syncthreads();
+    int slot = -1;
+    if (e >= 0) {
+      slot = next[e] + rank;
+#pragma unroll
+      for (int w = 0; w < WAVES - 1; ++w) slot += w < wave ? of_wave[w][e] : 0;
+    }
+    slots[tid] = slot;
+    if (tid < n) p.slot_of[t0 * p.k + tid] = slot;
+    __syncthreads();
+    if (tid < MAX_E)
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) next[tid] += of_wave[w][tid];
+    // The rows: a wavefront takes COPY times 64 chunks of a token's row at a time, of short rows several tokens'.
+    int shift = 6;                           // lanes to a row: a power of two
+    while (shift > 0 && p.chunks <= 1 << (shift - 1)) --shift;
+    const int side = 64 >> shift, column = lane & ((1 << shift) - 1);
+    const int parts = (p.chunks + (COPY << shift) - 1) / (COPY << shift);
+    for (int item = wave; item < ((tokens + side - 1) / side) * parts; item += WAVES) {
+      const int group = item / parts, part = item - group * parts;
+      const int token = group * side + (lane >> shift), c0 = part * (COPY << shift) + column;
+      if (token >= tokens) continue;
+      const u32x4* const from = (const u32x4*)p.x + (t0 + token) * p.chunks + c0;
+      u32x4 v[COPY];
+#pragma unroll
+      for (int q = 0; q < COPY; ++q)
+        if (c0 + (q << shift) < p.chunks) v[q] = from[q << shift];
+      for (int j = 0; j < p.k; ++j) {
+        const int to = slots[token * p.k + j];
+        if (to < 0) continue;
+        u32x4* const at = (u32x4*)p.rows + (int64_t)to * p.chunks + c0;
+#pragma unroll
+        for (int q = 0; q < COPY; ++q)
+          if (c0 + (q << shift) < p.chunks) at[q << shift] = v[q];
+      }
+    }
+    __syncthreads();                         // (`slots`, `next` and `of_wave` begin anew)
+  }
+}
+
+// ---- combine ---------------------------------------------------------------------------------------
+// Elements of a chunk: 4 fp32 or 8 bf16.
+template <typename S> struct Chunk;
+template <> struct Chunk<float> {
+  static constexpr int N = 4;
+  __device__ static float get(const u32x4& v, int j) { return __uint_as_float(v[j]); }
+  __device__ static u32x4 pack(const float (&x)[4]) {
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  }
+};
+template <> struct Chunk<uint16_t> {
+  static constexpr int N = 8;
+  __device__ static float get(const u32x4& v, int j) { return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16); }
+  __device__ static u32x4 pack(const float (&x)[8]) {              // (to the nearest, ties to even: the only rounding of a result)
+    u32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, bf16x2));
+    return v;
+  }
+};
+
+struct CombineArgs {
+  const char* y;                             // [R, H]
+  const int32_t* slot_of;                    // [T, k]; outside [0, R): not there
+  const float* weights;                      // [T, k], may be NULL (1)
+  int64_t T;
+  int k, chunks, R;
+  char* out;                                 // [T, H]
+  // backward
+  const char* dout;                          // [T, H]
+  char* dy;                                  // [R, H]
+  float* dweights;                           // [T, k], may be NULL: not wanted
+};
+
+// A thread takes one chunk of a token's row, KG slots' at once, so that their loads are in flight together; the sum goes in the slots' order.
+template <typename S, int KG>
+__global__ __launch_bounds__(THREADS) void combine_rows_kernel(CombineArgs p, int shift) {
+  constexpr int N = Chunk<S>::N;
+  const int lane = threadIdx.x & 63;
+  const int side = 64 >> shift, parts = (p.chunks + (1 << shift) - 1) >> shift;
+  const int64_t item = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
+  const int64_t group = item / parts;
+  const int64_t t = group * side + (lane >> shift);
+  const int c = (int)(item - group * parts) * (1 << shift) + (lane & ((1 << shift) - 1));
+  if (t >= p.T || c >= p.chunks) return;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = 0.f;
+  for (int j0 = 0; j0 < p.k; j0 += KG) {
+    int slot[KG];
+    float w[KG];
+    u32x4 v[KG];
+#pragma unroll
+    for (int j = 0; j < KG; ++j) {
+      slot[j] = j0 + j < p.k ? p.slot_of[t * p.k + j0 + j] : -1;
+      w[j] = j0 + j < p.k && p.weights ? p.weights[t * p.k + j0 + j] : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < KG; ++j)
+      if ((unsigned)slot[j] < (unsigned)p.R) v[j] = ((const u32x4*)p.y)[(int64_t)slot[j] * p.chunks + c];
+#pragma unroll
+    for (int j = 0; j < KG; ++j)
+      if ((unsigned)slot[j] < (unsigned)p.R)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = fmaf(w[j], Chunk<S>::get(v[j], i), sum[i]);
+  }
+  ((u32x4*)p.out)[t * p.chunks + c] = Chunk<S>::pack(sum);
+}
+
+// dy and dw of a token by 2^shift lanes, or by all of a workgroup of W wavefronts: each goes through its chunks of dout and of the k rows of y,
+// adding up k products in 32 bits, which are then joined in a fixed order.
+template <typename S, int KG, int W>
+__global__ __launch_bounds__(THREADS) void combine_rows_backward_kernel(CombineArgs p, int shift) {
+  constexpr int N = Chunk<S>::N, U = KG > 4 ? 1 : 2;
+  __shared__ float joined[WAVES][KG];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int side = W > 1 ? 1 : 64 >> shift;
+  const int64_t t = W > 1 ? (int64_t)blockIdx.x : ((int64_t)blockIdx.x * WAVES + wave) * side + (lane >> shift);
+  const int c0 = W > 1 ? threadIdx.x : lane & ((1 << shift) - 1), step = W > 1 ? THREADS : 1 << shift;
+  const bool mine = t < p.T;
+  for (int j0 = 0; j0 < p.k; j0 += KG) {
+    int slot[KG];
+    float w[KG], dot[KG];
+#pragma unroll
+    for (int j = 0; j < KG; ++j) {
+      const bool there = mine && j0 + j < p.k;
+      slot[j] = there ? p.slot_of[t * p.k + j0 + j] : -1;
+      if ((unsigned)slot[j] >= (unsigned)p.R) slot[j] = -1;
+      w[j] = there && p.weights ? p.weights[t * p.k + j0 + j] : 1.f;
+      dot[j] = 0.f;
+    }
+    if (mine)
+      for (int c = c0; c < p.chunks; c += U * step) {
+        u32x4 d[U], v[U][KG];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c + u * step < p.chunks) {
+            d[u] = ((const u32x4*)p.dout)[t * p.chunks + c + u * step];
+            if (p.dweights)
+#pragma unroll
+              for (int j = 0; j < KG; ++j)
+                if (slot[j] >= 0) v[u][j] = ((const u32x4*)p.y)[(int64_t)slot[j] * p.chunks + c + u * step];
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c + u * step < p.chunks) {
+#pragma unroll
+            for (int j = 0; j < KG; ++j)
+              if (slot[j] >= 0) {
+                float x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                  const float g = Chunk<S>::get(d[u], i);
+                  if (p.dweights) dot[j] = fmaf(g, Chunk<S>::get(v[u][j], i), dot[j]);
+                  x[i] = w[j] * g;
+                }
+                ((u32x4*)p.dy)[(int64_t)slot[j] * p.chunks + c + u * step] = Chunk<S>::pack(x);
+              }
+          }
+      }
+    if (!p.dweights) continue;
+#pragma unroll
+    for (int j = 0; j < KG; ++j)
+      for (int d = (W > 1 ? 64 : 1 << shift) >> 1; d > 0; d >>= 1) dot[j] += __shfl_xor(dot[j], d);
+    if (W > 1) {
+      if (j0) __syncthreads();
+      if (lane == 0)
+#pragma unroll
+        for (int j = 0; j < KG; ++j) joined[wave][j] = dot[j];
+      __syncthreads();
+      if (threadIdx.x == 0)
+#pragma unroll
+        for (int j = 0; j < KG; ++j) dot[j] = (joined[0][j] + joined[1][j]) + (joined[2][j] + joined[3][j]);
+    }
+    if (mine && c0 == 0)
+#pragma unroll
+      for (int j = 0; j < KG; ++j)
+        if (j0 + j < p.k) p.dweights[t * p.k + j0 + j] = dot[j];
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+int check_rows_shape(const char* who, int64_t T, int k, int H, moep_dtype dt) {
+  if (dt != MOEP_F32 && dt != MOEP_BF16) return fail(MOEP_EINVAL, "%s: unknown dtype %d", who, (int)dt);
+  if (k < 1 || k > MAX_K) return fail(MOEP_EINVAL, "%s: k=%d out of range [1, %d]", who, k, MAX_K);
+  if (T < 0 || T > ((int64_t)1 << 30) / k) return fail(MOEP_EINVAL, "%s: T=%lld out of range [0, 2^30 / k]", who, (long long)T);
+  if (H < 1 || H > 1 << 24) return fail(MOEP_EINVAL, "%s: H=%d out of range [1, 2^24]", who, H);
+  if (H % (dt == MOEP_BF16 ? 64 : 4)) return fail(MOEP_EUNSUPPORTED, "%s: H=%d must be a multiple of %d", who, H, dt == MOEP_BF16 ? 64 : 4);
+  return MOEP_OK;
+}
+int check_16(const char* who, std::initializer_list<const void*> pointers) {
+  for (const void* q : pointers)
+    if ((uintptr_t)q & 15) return fail(MOEP_EUNSUPPORTED, "%s: rows must be 16-byte aligned", who);
+  return MOEP_OK;
+}
+int check_4(const char* who, std::initializer_list<const void*> pointers) {
+  for (const void* q : pointers)
+    if ((uintptr_t)q & 3) return fail(MOEP_EUNSUPPORTED, "%s: slots, experts, offsets and weights must be 4-byte aligned", who);
+  return MOEP_OK;
+}
+
+// Slots up to which every workgroup counts all ids by itself, in one launch.
+constexpr int64_t ONE_LAUNCH_SLOTS = 8192;
+constexpr int64_t MIN_PIECE = 1024, MAX_PIECES = 512;
+struct DispatchPlan { int64_t piece = 0; int pieces = 0; int per = 1; };
+DispatchPlan plan_dispatch(int64_t T, int k) {
+  DispatchPlan p;
+  if (T * k <= ONE_LAUNCH_SLOTS) {
+    p.per = (int)ceil_div(T, 1024) > 1 ? (int)ceil_div(T, 1024) : 1;
+    return p;
+  }
+  p.per = 16;
+  while (p.per < 1024 && T / p.per > 16384) p.per *= 2;
+  p.piece = ceil_div(ceil_div(T, MAX_PIECES), 1024) * 1024;      // (a multiple of every `per`)
+  if (p.piece < MIN_PIECE) p.piece = MIN_PIECE;
+  p.pieces = (int)ceil_div(T, p.piece);
+  return p;
+}
+
+int row_shift(int chunks) {                  // lanes to a row, as a power of two
+  int s = 6;
+  while (s > 0 && chunks <= 1 << (s - 1)) --s;
+  return s;
+}
+
+template <typename F>
+void with_slots(int k, F launch) {
+  if (k == 1) launch(std::integral_constant<int, 1>{});
+  else if (k == 2) launch(std::integral_constant<int, 2>{});
+  else if (k <= 4) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 8>{});
+}
+
+int launch_combine(const CombineArgs& p, moep_dtype dt, hipStream_t s, const char* name) {
+  const int shift = row_shift(p.chunks), side = 64 >> shift;
+  const int64_t parts = ceil_div(p.chunks, 1 << shift), tokens = ((int64_t)1 << 23) / parts * side;   // of a launch
+  Timed timed(name, s);
+  const int64_t row = (int64_t)p.chunks * 16;
+  for (int64_t t = 0; t < p.T; t += tokens) {
+    CombineArgs a = p;
+    a.T = p.T - t < tokens ? p.T - t : tokens;
+    a.slot_of += t * p.k;
+    if (a.weights) a.weights += t * p.k;
+    a.out += t * row;
+    const unsigned blocks = (unsigned)ceil_div(ceil_div(a.T, side) * parts, WAVES);
+    with_slots(p.k, [&](auto kg) {
+      constexpr int KG = decltype(kg)::value;
+      if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_kernel<uint16_t, KG>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+      else hipLaunchKernelGGL((combine_rows_kernel<float, KG>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+    });
+    MOEP_HIP(hipGetLastError());
+  }
+  return MOEP_OK;
+}
+
+}  // namespace
+}  // namespace moep
+
+using namespace moep;
+
+extern "C" {
+
+size_t moe_dispatch_rows_workspace(int64_t T, int k, int E) {
+  if (k < 1 || k > MAX_K || E < 1 || E > MAX_E || T < 0 || T > ((int64_t)1 << 30) / k) return 0;
+  return (size_t)plan_dispatch(T, k).pieces * E * sizeof(int32_t);
+}
+
+int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used, int64_t T, int k, int E, int H, moep_dtype dt, void* rows,
+                      int32_t* slot_of, int32_t* offsets, void* ws, size_t ws_bytes, void* hip_stream) {
+  const char* who = "moe_dispatch_rows";
+  if (int st = check_rows_shape(who, T, k, H, dt)) return st;
+  if (E < 1 || E > MAX_E) return fail(MOEP_EINVAL, "%s: E=%d out of range [1, %d]", who, E, MAX_E);
+  if (!offsets) return fail(MOEP_EINVAL, "%s: NULL offsets", who);
+  if (T > 0 && (!x || !experts || !rows || !slot_of)) return fail(MOEP_EINVAL, "%s: NULL x, experts, rows or slot_of", who);
+  if (int st = check_16(who, {x, rows})) return st;
+  if (int st = check_4(who, {experts, used, slot_of, offsets})) return st;
+  const size_t need = moe_dispatch_rows_workspace(T, k, E);
+  if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
+    return fail(MOEP_EWORKSPACE, "%s: needs a 256-byte aligned workspace of %zu bytes", who, need);
+  hipStream_t s = (hipStream_t)hip_stream;
+  const DispatchPlan plan = plan_dispatch(T, k);
+  DispatchArgs p = {(const char*)x, experts, used, T, k, E, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), plan.per,
+                    plan.pieces ? (int32_t*)ws : nullptr, plan.piece, plan.pieces, (char*)rows, slot_of, offsets};
+  if (plan.pieces) {
+    Timed timed("count_rows", s);
+    hipLaunchKernelGGL(count_rows_kernel, dim3((unsigned)plan.pieces), dim3(THREADS), 0, s, p);
+    MOEP_HIP(hipGetLastError());
+  }
+  Timed timed("dispatch_rows", s);
+  hipLaunchKernelGGL(dispatch_rows_kernel, dim3((unsigned)(T > 0 ? ceil_div(T, plan.per) : 1)), dim3(THREADS), 0, s, p);
+  MOEP_HIP(hipGetLastError());
+  return MOEP_OK;
+}
+
+int moe_dispatch_rows_backward(const void* drows, const int32_t* slot_of, int64_t T, int k, int H, int64_t R, moep_dtype dt, void* dx,
+                               void* hip_stream) {
+  const char* who = "moe_dispatch_rows_backward";
+  if (int st = check_rows_shape(who, T, k, H, dt)) return st;
+  if (R < 0 || R > (int64_t)1 << 30) return fail(MOEP_EINVAL, "%s: R=%lld out of range [0, 2^30]", who, (long long)R);
+  if (T == 0) return MOEP_OK;
+  if ((!drows && R > 0) || !slot_of || !dx) return fail(MOEP_EINVAL, "%s: NULL drows, slot_of or dx", who);
+  if (int st = check_16(who, {drows, dx})) return st;
+  if (int st = check_4(who, {slot_of})) return st;
+  CombineArgs p = {(const char*)drows, slot_of, nullptr, T, k, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), (int)R, (char*)dx, nullptr, nullptr, nullptr};
+  return launch_combine(p, dt, (hipStream_t)hip_stream, "dispatch_rows_backward");
+}
+
+int moe_combine_rows(const void* y, const int32_t* slot_of, const float* weights, int64_t T, int k, int H, int64_t R, moep_dtype dt, void* out,
+                     void* hip_stream) {
+  const char* who = "moe_combine_rows";
+  if (int st = check_rows_shape(who, T, k, H, dt)) return st;
+  if (R < 0 || R > (int64_t)1 << 30) return fail(MOEP_EINVAL, "%s: R=%lld out of range [0, 2^30]", who, (long long)R);
+  if (T == 0) return MOEP_OK;
+  if ((!y && R > 0) || !slot_of || !out) return fail(MOEP_EINVAL, "%s: NULL y, slot_of or out", who);
+  if (int st = check_16(who, {y, out})) return st;
+  if (int st = check_4(who, {slot_of, weights})) return st;
+  CombineArgs p = {(const char*)y, slot_of, weights, T, k, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), (int)R, (char*)out, nullptr, nullptr, nullptr};
+  return launch_combine(p, dt, (hipStream_t)hip_stream, "combine_rows");
+}
+
+int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* slot_of, const float* weights, int64_t T, int k, int H, int64_t R,
+                              moep_dtype dt, void* dy, float* dweights, void* hip_stream) {
+  const char* who = "moe_combine_rows_backward";
+  if (int st = check_rows_shape(who, T, k, H, dt)) return st;
+  if (R < 0 || R > (int64_t)1 << 30) return fail(MOEP_EINVAL, "%s: R=%lld out of range [0, 2^30]", who, (long long)R);
+  if (T == 0) return MOEP_OK;
+  if (!dout || !slot_of || (!dy && R > 0)) return fail(MOEP_EINVAL, "%s: NULL dout, slot_of or dy", who);
+  if (dweights && !y && R > 0) return fail(MOEP_EINVAL, "%s: the weights' gradient needs y", who);
+  if (int st = check_16(who, {dout, y, dy})) return st;
+  if (int st = check_4(who, {slot_of, weights, dweights})) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const CombineArgs p = {(const char*)y, slot_of, weights, T, k, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), (int)R, nullptr, (const char*)dout,
+                         (char*)dy, dweights};
+  const int shift = row_shift(p.chunks);
+  const bool wide = p.chunks > 64 && T <= 2048;                    // a workgroup to a token
+  const int64_t each = wide ? 1 : (int64_t)WAVES * (64 >> shift), tokens = each << 20;
+  Timed timed("combine_rows_backward", s);
+  const int64_t row = (int64_t)p.chunks * 16;
+  for (int64_t t = 0; t < T; t += tokens) {
+    CombineArgs a = p;
+    a.T = T - t < tokens ? T - t : tokens;
+    a.slot_of += t * k;
+    if (a.weights) a.weights += t * k;
+    a.dout += t * row;
+    if (a.dweights) a.dweights += t * k;
+    const unsigned blocks = (unsigned)ceil_div(a.T, each);
+    with_slots(k, [&](auto kg) {
+      constexpr int KG = decltype(kg)::value;
+      auto with = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_backward_kernel<uint16_t, KG, W>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+        else hipLaunchKernelGGL((combine_rows_backward_kernel<float, KG, W>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+      };
+      if (wide) with(std::integral_constant<int, WAVES>{});
+      else with(std::integral_constant<int, 1>{});
+    });
+    MOEP_HIP(hipGetLastError());
+  }
+  return MOEP_OK;
+}
+
+}  // extern "C"
