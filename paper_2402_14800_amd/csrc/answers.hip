@@ -30,6 +30,8 @@ struct AnswerArgs {
   float* loss; float* logprob;
   float* stats;                              // [T, 3]: m, log s, c (GRADIENT reads them)
   void* grad; int64_t ld_grad;
+  int64_t stream_rows;                       // the launch's first rows are read past the caches: so many of them
+  bool stream_grad;                          // and the gradient is written past them
 };
 
 // exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, 1e-9 of the sum.)
@@ -83,20 +85,119 @@ __device__ __forceinline__ int answer_of(const int64_t* offsets, int n, int64_t 
   return lo - 1;
 }
 
+// ---- a row's statistics, where the row is not used again -------------------------------------------
+// Four chunks at a time, the next four on their way meanwhile, each four with a running maximum of its own: a wavefront adds up what has
+// come while the rest comes, and 32 registers of chunks leave room for twice as many wavefronts as a row that is held.  An element costs
+// the lanes seven operations (unpacked, one FMA, the exponential's four, one sum): the exponent is z c - k with k the integer next to m c, whose
+// factor exp2(k - m c) is left to the four's sum.
+constexpr int GROUP = 4;
+struct Running {
+  float m = NEG_INF, s = 0.f;                // maximum, and sum of exp2((z - m) c)
+  float k = 0.f, f = 1.f;                    // k: integer next to m c, f = exp2(k - m c)
+  bool near = true;                          // |m c| < 2^20: k is as exact as the exponents need it
+};
+// (by name: of an array the compiler kept parts in memory)
+struct Group {
+  u32x4 a, b, c, d;
+  template <typename F> __device__ __forceinline__ void each(F f) { f(a, 0); f(b, 1); f(c, 2); f(d, 3); }
+};
+template <typename S, int B>
+__device__ __forceinline__ void request_group(const Row<S>& row, int g, int tid, bool stream, Group& v) {
+  if (stream) {
+    apart();
+    v.each([&](u32x4& x, int n) { request<true>(row, (g * GROUP + n) * B + tid, x); });
+    apart();
+  } else v.each([&](u32x4& x, int n) { request(row, (g * GROUP + n) * B + tid, x); });
+}
+template <typename S>
+__device__ __forceinline__ float largest_of(Group& v) {
+  constexpr int N = Elements<S>::N;
+  if constexpr (sizeof(S) == 2) {            // (as in `largest`)
+    const s16x2 top = __builtin_elementwise_max(__builtin_elementwise_max(top_halves(v.a), top_halves(v.b)),
+                                                __builtin_elementwise_max(top_halves(v.c), top_halves(v.d)));
+    const short x = max(top[0], top[1]);
+    if (x >= 0) return __uint_as_float((unsigned)x << 16);
+  }
+  float m = NEG_INF;
+  v.each([&](u32x4& x, int) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) m = max_nan(m, Elements<S>::get(x, j));
+  });
+  return m;
+}
+template <typename S>
+__device__ __forceinline__ void add_group(Group& v, Running& a, float c) {
+  constexpr int N = Elements<S>::N;
+  const float m = max_nan(a.m, largest_of<S>(v));
+  v.each([](u32x4& x, int) { asm volatile("" : "+v"(x)); });           // (taken apart anew, not held taken apart: see use_again)
+  if (!(m == a.m)) {
+    a.s = moved<false>(Stats{a.m, a.s, 0.f}, m, c).s;
+    a.m = m;
+    a.near = fabsf(m * c) < 0x1p20f;
+    a.k = a.near ? rintf(m * c) : 0.f;
+    a.f = a.near ? exp2_fast(a.k - m * c) : 1.f;
+  }
+  float s0 = 0.f, s1 = 0.f;
+  auto add = [&](auto exponent) {
+    v.each([&](u32x4& x, int) {
+#pragma unroll
+      for (int j = 0; j < N; j += 2) {
+        s0 += exp2_fast(exponent(Elements<S>::get(x, j)));
+        s1 += exp2_fast(exponent(Elements<S>::get(x, j + 1)));
+      }
+    });
+  };
+  const float r = reference(m);
+  if (a.near) add([&](float z) { return fmaf(z, c, -a.k); });
+  else add([&](float z) { return (z - r) * c; });            // nothing but -inf so far, logits near the type's ends, or a cold temperature
+  a.s = fmaf(s0 + s1, a.f, a.s);
+}
+// The group's chunks that reach beyond the row cut to it: the row's first and last one, in the threads that hold them.
+template <typename S, int B>
+__device__ __forceinline__ void cut_group(const Row<S>& row, int g, int tid, Group& v) {
+  const int c0 = g * (GROUP * B), last = row.chunks - 1;
+  if (row.lead && c0 + tid == 0) v.a = cut(row, 0, v.a);
+  if (!row.whole(last) && last >= c0 && last < c0 + GROUP * B && (last - c0) % B == tid && !(row.lead && last == 0)) {
+    u32x4 end = v.a;
+    v.each([&](u32x4& x, int n) { if (c0 + n * B + tid == last) end = x; });
+    end = cut(row, last, end);
+    v.each([&](u32x4& x, int n) { if (c0 + n * B + tid == last) x = end; });
+  }
+}
+template <typename S, int B>
+__device__ __forceinline__ Stats add_row(const Row<S>& row, int tid, float c, bool stream) {
+  const int groups = (row.chunks + GROUP * B - 1) / (GROUP * B);
+  Running a;
+  Group now, then;
+  request_group<S, B>(row, 0, tid, stream, now);
+  request_group<S, B>(row, 1, tid, stream, then);
+  for (int g = 0; g < groups; g += 2) {
+    cut_group<S, B>(row, g, tid, now);
+    add_group<S>(now, a, c);
+    request_group<S, B>(row, g + 2, tid, stream, now);
+    if (g + 1 >= groups) break;              // (the same for all threads)
+    cut_group<S, B>(row, g + 1, tid, then);
+    add_group<S>(then, a, c);
+    request_group<S, B>(row, g + 3, tid, stream, then);
+  }
+  return Stats{a.m, a.s, 0.f};
+}
+
 // HELD: the row fits the workgroup's registers (LOSS_AND_GRADIENT, the one mode that uses a row twice).
 template <typename S, int B, int MODE, bool HELD>
-__global__ __launch_bounds__(B) void answers_kernel(AnswerArgs p) {
+__global__ __launch_bounds__(B, MODE == LOSS ? 7 : 1) void answers_kernel(AnswerArgs p) {
   constexpr int N = Elements<S>::N;
   __shared__ float shared[3 * (B / 64)];
   int tid = threadIdx.x;
-  // (a pair's gradient: the rows that the loss read last are the ones that the caches still hold)
-  const int64_t t = MODE == GRADIENT && p.offsets ? p.T - 1 - blockIdx.x : blockIdx.x;
+  // (the gradient by itself: the rows that the loss read last are the ones that the caches still hold)
+  const int64_t t = MODE == GRADIENT ? p.T - 1 - blockIdx.x : blockIdx.x;
+  const bool stream = MODE != GRADIENT && t < p.stream_rows, stream_grad = MODE == GRADIENT || p.stream_grad;
   const Row<S> row(p.logits, p.ld, p.V, t, p.T);
   const int tiles = HELD ? 1 : (row.chunks + B * NC - 1) / (B * NC);
   S* const out = MODE == LOSS ? nullptr : (S*)p.grad + t * p.ld_grad;
   const bool aligned = (((uintptr_t)out ^ (uintptr_t)row.at) & 15) == 0;
   auto write_zeros = [&]() {
-    for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0});
+    for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0}, stream_grad);
   };
   const int64_t y = p.tokens[t];
   const float c = uniform(LOG2E / p.tau);
@@ -122,11 +223,18 @@ __global__ __launch_bounds__(B) void answers_kernel(AnswerArgs p) {
       if (p.ref) ref = p.ref[t];
     }
     Stats all = {NEG_INF, 0.f, 0.f};
-    for (int i = 0; i < tiles; ++i) {
-      tid = thread_again(tid);
-      request_tile<S, B>(row, i, tid, v);
-      cut_ends<S, B>(row, i, tid, v);
-      add_tile<S, B, false>(v, row.chunks - i * (B * NC), all, c);
+    if (!HELD) {
+      all = add_row<S, B>(row, tid, c, stream);
+    } else {
+      if (stream) {
+        apart();
+        request_tile<S, B, true>(row, 0, tid, v);
+        apart();
+      } else {
+        request_tile<S, B>(row, 0, tid, v);
+      }
+      cut_ends<S, B>(row, 0, tid, v);
+      add_tile<S, B, false>(v, row.chunks, all, c);
     }
     zy = uniform(zy);                                        // (here before anybody writes: grad may be the logits' own memory)
     all = join_wave<B, false>(all, c, shared);
@@ -191,7 +299,7 @@ __global__ __launch_bounds__(B) void answers_kernel(AnswerArgs p) {
         if (at == at_y)
 #pragma unroll
           for (int j = 0; j < N; ++j) x[j] += j == of_y ? scale : 0.f;
-        store_chunk(row, out, aligned, at, Elements<S>::pack(x));
+        store_chunk(row, out, aligned, at, Elements<S>::pack(x), stream_grad);
       }
     }
   }
@@ -200,34 +308,40 @@ __global__ __launch_bounds__(B) void answers_kernel(AnswerArgs p) {
 // A pair: both answers' sums of lp - ref in 64 bits, the loss, the rewards, and c of every row of theirs.
 struct PairArgs {
   const int64_t* tokens; const int64_t* offsets; const float* ref; const float* logprob;
-  int64_t T, pairs, first;                   // `first`: of the launch
+  int64_t T, pairs;
   float beta, smoothing;
   int average;
   float* loss; float* rewards; float* stats;
 };
-constexpr int PAIR_THREADS = 256;
+constexpr int PAIR_THREADS = 512, SIDE_WAVES = PAIR_THREADS / 128;    // half of the threads to an answer
+static_assert(SIDE_WAVES == 4, "four sums are added below");
 
 __global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
-  __shared__ double sums[2][PAIR_THREADS / 64];
-  __shared__ int64_t given[2][PAIR_THREADS / 64];
-  const int tid = threadIdx.x;
-  const int64_t pair = p.first + blockIdx.x;
-  int64_t r0[2], r1[2];
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const int64_t a = side ? p.pairs + pair : pair;
-    r0[side] = max((int64_t)0, min(p.T, p.offsets[a]));
-    r1[side] = max((int64_t)0, min(p.T, p.offsets[a + 1]));
-  }
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
+  __shared__ double sums[2][SIDE_WAVES];
+  __shared__ int64_t given[2][SIDE_WAVES];
+  const int side = threadIdx.x >= PAIR_THREADS / 2 ? 1 : 0, tid = threadIdx.x & (PAIR_THREADS / 2 - 1);
+  const int64_t pair = blockIdx.x;
+  const int64_t* const at = p.offsets + (side ? p.pairs + pair : pair);
+  const int64_t r0 = max((int64_t)0, min(p.T, at[0])), r1 = max((int64_t)0, min(p.T, at[1]));
+  {
     double x = 0;
     int64_t n = 0;
-    for (int64_t t = r0[side] + tid; t < r1[side]; t += PAIR_THREADS)
-      if (p.tokens[t] >= 0) {
-        x += (double)p.logprob[t] - (double)p.ref[t];
-        ++n;
+    constexpr int DEEP = 4;
+    for (int64_t t = r0 + tid; t < r1; t += DEEP * (PAIR_THREADS / 2)) {
+      int64_t y[DEEP];
+      float lp[DEEP], ref[DEEP];
+#pragma unroll
+      for (int q = 0; q < DEEP; ++q) {       // (beyond the end the last row again: all loads at once)
+        const int64_t i = min(t + q * (PAIR_THREADS / 2), r1 - 1);
+        y[q] = p.tokens[i]; lp[q] = p.logprob[i]; ref[q] = p.ref[i];
       }
+#pragma unroll
+      for (int q = 0; q < DEEP; ++q)
+        if (t + q * (PAIR_THREADS / 2) < r1 && y[q] >= 0) {
+          x += (double)lp[q] - (double)ref[q];
+          ++n;
+        }
+    }
     for (int d = 32; d > 0; d >>= 1) {
       x += __shfl_xor(x, d);
       n += __shfl_xor(n, d);
@@ -237,40 +351,43 @@ __global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
   __syncthreads();
   double reward[2], by[2];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const double x = (sums[side][0] + sums[side][1]) + (sums[side][2] + sums[side][3]);
-    const int64_t n = given[side][0] + given[side][1] + given[side][2] + given[side][3];
-    by[side] = (double)p.beta / (double)(p.average && n > 0 ? n : 1);
-    reward[side] = by[side] * x;
+  for (int a = 0; a < 2; ++a) {
+    const double x = (sums[a][0] + sums[a][1]) + (sums[a][2] + sums[a][3]);
+    const int64_t n = given[a][0] + given[a][1] + given[a][2] + given[a][3];
+    by[a] = (double)p.beta / (double)(p.average && n > 0 ? n : 1);
+    reward[a] = by[a] * x;
   }
   const double h = reward[0] - reward[1], ls = (double)p.smoothing;
-  // -log sigmoid(h) = max(-h, 0) + log(1 + exp(-|h|)), and the other one is h more
-  const double away = log1p(exp(-fabs(h)));
-  const double loss = (1 - ls) * (fmax(-h, 0.0) + away) + (ls > 0 ? ls * (fmax(h, 0.0) + away) : 0.0);
-  const double by_h = ls - 1 / (1 + exp(h));
-  if (tid == 0) {
+  const double e = exp(-fabs(h)), by_h = ls - (h > 0 ? e : 1.0) / (1 + e);
+  const float c = (float)((side ? -by_h : by_h) * by[side]);
+  for (int64_t t = r0 + tid; t < r1; t += PAIR_THREADS / 2) p.stats[3 * t + 2] = p.tokens[t] >= 0 ? c : 0.f;
+  if (threadIdx.x == 0) {
+    // -log sigmoid(h) = max(-h, 0) + log(1 + exp(-|h|)), and the other one is h more
+    const double away = log1p(e);
+    const double loss = (1 - ls) * (fmax(-h, 0.0) + away) + (ls > 0 ? ls * (fmax(h, 0.0) + away) : 0.0);
     p.loss[pair] = (float)(h == h ? loss : h);
     p.rewards[pair] = (float)reward[0];
     p.rewards[p.pairs + pair] = (float)reward[1];
   }
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const float c = (float)((side ? -by_h : by_h) * by[side]);
-    for (int64_t t = r0[side] + tid; t < r1[side]; t += PAIR_THREADS) p.stats[3 * t + 2] = p.tokens[t] >= 0 ? c : 0.f;
-  }
 }
 
+constexpr double CACHE_BYTES = 268e6, STREAM_BYTES = 134e6, KEPT_BYTES = 160e6;
 template <int MODE>
 int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
   const int64_t chunks = most_chunks(whole.logits, whole.ld, whole.V, dt);
   const int threads = MODE == LOSS ? threads_to_read(T, chunks) : threads_to_hold(T, chunks);
+  const double bytes = (double)whole.V * (double)dtype_size(dt);       // of a row
+  // rows of the loss alone in front of those that the caches can keep for the gradient; all of a large batch whose gradient comes with it
+  const int64_t streamed = MODE == LOSS ? T - (int64_t)(KEPT_BYTES / bytes) : bytes * (double)T > STREAM_BYTES ? T : 0;
   Timed timed(name, s);
   const int64_t launches = ceil_div(T, LAUNCH_ROWS);
   for (int64_t i = 0; i < launches; ++i) {
-    const int64_t t = (MODE == GRADIENT && whole.offsets ? launches - 1 - i : i) * LAUNCH_ROWS;
+    const int64_t t = (MODE == GRADIENT ? launches - 1 - i : i) * LAUNCH_ROWS;
     AnswerArgs p = whole;
     p.T = T - t < LAUNCH_ROWS ? T - t : LAUNCH_ROWS;
     p.first = t;
+    p.stream_rows = streamed - t;
+    p.stream_grad = bytes * (double)T > CACHE_BYTES;
     const int64_t size = (int64_t)dtype_size(dt);
     p.logits = (const char*)whole.logits + t * whole.ld * size;
     p.tokens += t;
@@ -382,7 +499,7 @@ int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, c
     if (int st = launch_answers<LOSS>(p, T, dt, s, "answer_logprobs")) return st;
   if (pairs > 0) {
     Timed timed("pairs", s);
-    const PairArgs q = {tokens, offsets, ref_logprob, logprob, T, pairs, 0, beta, smoothing, average, loss, rewards, stats};
+    const PairArgs q = {tokens, offsets, ref_logprob, logprob, T, pairs, beta, smoothing, average, loss, rewards, stats};
     hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)pairs), dim3(PAIR_THREADS), 0, s, q);
     MOEP_HIP(hipGetLastError());
   }

@@ -84,17 +84,20 @@ __device__ __forceinline__ u32x4 neutral() {
   return u32x4{Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL, Elements<S>::NEUTRAL};
 }
 
-// Chunk c (thread by thread) of a row: the request alone, nothing waits.  What is not there is -inf.
-template <typename S>
+// Between two branches that differ in a hint to the caches alone: the compiler would make one of both, without the hint.
+__device__ __forceinline__ void apart() { asm volatile(""); }
+
+// Chunk c (thread by thread) of a row: the request alone, nothing waits.  What is not there is -inf.  STREAM: past the caches.
+template <bool STREAM = false, typename S>
 __device__ __forceinline__ void request(const Row<S>& row, int c, u32x4& v) {
   v = neutral<S>();
-  if (c >= row.first_load && c < row.end_load) v = *row.chunk(c);
+  if (c >= row.first_load && c < row.end_load) v = STREAM ? __builtin_nontemporal_load(row.chunk(c)) : *row.chunk(c);
 }
 // Chunks tile B NC + n B + tid of a row
-template <typename S, int B>
+template <typename S, int B, bool STREAM = false>
 __device__ __forceinline__ void request_tile(const Row<S>& row, int tile, int tid, u32x4 (&v)[NC]) {
 #pragma unroll
-  for (int n = 0; n < NC; ++n) request(row, tile * (B * NC) + n * B + tid, v[n]);
+  for (int n = 0; n < NC; ++n) request<STREAM>(row, tile * (B * NC) + n * B + tid, v[n]);
 }
 // The thread's index as a number that the compiler knows nothing of.  Taken anew for every row: what it can tell ahead of all rows (sixteen
 // offsets, sixteen comparisons' sides) it keeps in registers from row to row.
@@ -271,10 +274,16 @@ __device__ __forceinline__ Stats join_all(const Stats& a, float c, const float* 
 // `aligned`: whether the gradient's row starts like the logits' within 16 bytes.  Else all of a chunk's elements are stored by themselves:
 // loss and gradient of 4096 rows of 32000 bf16 in rows of 32001, the gradient in rows of 32000, 225 us for 122, the gradient alone 215 for 122.
 template <typename S>
-__device__ __forceinline__ void store_chunk(const Row<S>& row, S* out, bool aligned, int c, u32x4 v) {
+__device__ __forceinline__ void store_chunk(const Row<S>& row, S* out, bool aligned, int c, u32x4 v, bool stream = false) {
   const int i0 = c * Row<S>::N - row.lead;
   if (aligned && row.whole(c)) {
-    *(u32x4*)(out + i0) = v;
+    if (stream) {                                            // (past the caches)
+      apart();
+      __builtin_nontemporal_store(v, (u32x4*)(out + i0));
+      apart();
+    } else {
+      *(u32x4*)(out + i0) = v;
+    }
     return;
   }
 #pragma unroll 1

@@ -35,16 +35,24 @@ struct DispatchArgs {
   int32_t* offsets;                          // [E + 1]
 };
 
-// The expert of slot i = t k + j, -1 if the slot is not used.
-__device__ __forceinline__ int expert_at(const DispatchArgs& p, unsigned i) {
-  const int e = p.experts[i];
-  bool there = (unsigned)e < (unsigned)p.E;
-  if (p.used) {
-    const unsigned t = i / (unsigned)p.k;
-    there = there && (int)(i - t * (unsigned)p.k) < p.used[t];
+// Slots i, i + THREADS, .. as they are in memory (beyond `end` slot end - 1 again: all loads at once, and no lane's waits for another's),
+// and the expert of each: -1 if the slot is not used, or beyond the end.
+template <int DEEP>
+struct Ids {
+  int expert[DEEP], used[DEEP];
+  __device__ __forceinline__ void request(const DispatchArgs& p, unsigned i, unsigned end) {
+#pragma unroll
+    for (int q = 0; q < DEEP; ++q) expert[q] = p.experts[min(i + q * THREADS, end - 1)];
+    if (p.used)
+#pragma unroll
+      for (int q = 0; q < DEEP; ++q) used[q] = p.used[min(i + q * THREADS, end - 1) / (unsigned)p.k];
   }
-  return there ? e : -1;
-}
+  __device__ __forceinline__ int at(const DispatchArgs& p, int q, unsigned i, unsigned end) const {
+    bool there = i + q * THREADS < end && (unsigned)expert[q] < (unsigned)p.E;
+    if (p.used) there = there && (int)((i + q * THREADS) % (unsigned)p.k) < used[q];
+    return there ? expert[q] : -1;
+  }
+};
 
 // Counts in LDS, eight copies so that the lanes of a wavefront seldom meet at one.
 constexpr int COPIES = 8;
@@ -58,16 +66,18 @@ __device__ __forceinline__ int total(const Counts& c, int e) {
   for (int q = 0; q < COPIES; ++q) n += c.n[q][e];
   return n;
 }
-// Adds the ids of slots i0 .. i1 - 1, eight of a thread's in flight.
-__device__ __forceinline__ void count(const DispatchArgs& p, unsigned i0, unsigned i1, Counts* c) {
-  int* const mine = c->n[threadIdx.x & (COPIES - 1)];
-  for (unsigned i = i0 + threadIdx.x; i < i1; i += 8 * THREADS) {
-    int e[8];
+// Adds the ids of slots i0 .. i1 - 1, those in front of `split` to `a`, the others to `b`.
+__device__ __forceinline__ void count(const DispatchArgs& p, unsigned i0, unsigned split, unsigned i1, Counts* a, Counts* b) {
+  const int copy = threadIdx.x & (COPIES - 1);
+  constexpr int DEEP = 16;
+  for (unsigned i = i0 + threadIdx.x; i < i1; i += DEEP * THREADS) {
+    Ids<DEEP> ids;
+    ids.request(p, i, i1);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) e[q] = i + q * THREADS < i1 ? expert_at(p, i + q * THREADS) : -1;
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (e[q] >= 0) atomicAdd(&mine[e[q]], 1);
+    for (int q = 0; q < DEEP; ++q) {
+      const int e = ids.at(p, q, i, i1);
+      if (e >= 0) atomicAdd(&(i + q * THREADS < split ? a : b)->n[copy][e], 1);
+    }
   }
 }
 
@@ -76,66 +86,96 @@ __global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
   clear(&c);
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
-  count(p, (unsigned)(t0 * p.k), (unsigned)(t1 * p.k), &c);
+  count(p, (unsigned)(t0 * p.k), (unsigned)(t1 * p.k), (unsigned)(t1 * p.k), &c, &c);
   __syncthreads();
   if ((int)threadIdx.x < p.E) p.counts[(int64_t)blockIdx.x * p.E + threadIdx.x] = total(c, threadIdx.x);
 }
 
-// Chunks of a row that a wavefront's lanes bring at once, a multiple of 64 of them.
+// The rows: a wavefront takes COPY times 64 chunks of a token's row at a time, of short rows several tokens'.
 constexpr int COPY = 4;
+struct Piece {
+  u32x4 v[COPY];
+  int token, c0;
+};
 
-__global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p) {
-  __shared__ Counts before, rest;
+__global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p, int shift) {
+  __shared__ Counts before, rest, twice;
   __shared__ int next[MAX_E];                // the number of the next row of each expert
   __shared__ int of_wave[WAVES][MAX_E];
   __shared__ int slots[THREADS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t first = (int64_t)blockIdx.x * p.per, last = min(p.T, first + p.per);
+  const unsigned i_first = (unsigned)(first * p.k), i_all = (unsigned)(p.T * p.k);
+  // (2^shift lanes to a row)
+  const int side = 64 >> shift, parts = (p.chunks + (COPY << shift) - 1) / (COPY << shift);
+  const int batch = THREADS / p.k;           // tokens whose slots are worked out at once, one to a thread
+  auto bring = [&](int64_t t0, int tokens, int item, Piece& x) {
+    const int group = item / parts;
+    x.token = group * side + (lane >> shift);
+    x.c0 = (item - group * parts) * (COPY << shift) + (lane & ((1 << shift) - 1));
+    const u32x4* const from = (const u32x4*)p.x + (t0 + x.token) * p.chunks + x.c0;
+#pragma unroll
+    for (int q = 0; q < COPY; ++q)
+      if (x.token < tokens && x.c0 + (q << shift) < p.chunks) x.v[q] = from[q << shift];
+  };
+  // (what the first batch needs is asked for before the counting, which takes longer than it)
+  Ids<1> ids;
+  Piece piece;
+  if (first < last) {
+    const int tokens = (int)min((int64_t)batch, last - first);
+    ids.request(p, i_first + tid, i_first + tokens * p.k);
+    bring(first, tokens, wave, piece);
+  }
   clear(&before);
   clear(&rest);
+  clear(&twice);
   __syncthreads();
   if (p.counts) {
-    const int64_t mine = first / p.piece;    // (a workgroup's tokens lie in one piece)
-    for (int i = tid; i < p.pieces * p.E; i += THREADS) {
-      const int n = p.counts[i], c = i / p.E, e = i - c * p.E;
-      if (n) atomicAdd(&(c < mine ? before : rest).n[tid & (COPIES - 1)][e], n);
-    }
-    // (of the piece's own ids those in front of the workgroup's belong to `before`, and are counted in `rest` as well: taken off below)
-    __shared__ Counts twice;
-    clear(&twice);
-    __syncthreads();
-    count(p, (unsigned)(mine * p.piece * p.k), (unsigned)(first * p.k), &twice);
-    __syncthreads();
-    if (tid < p.E) {
-      const int n = total(twice, tid);
-      before.n[0][tid] += n;
-      rest.n[0][tid] -= n;
+    // pieces in front of the workgroup's (its tokens lie in one), and all others; of its own the ids in front of the workgroup's, which
+    // are counted among the others as well
+    const int mine = (int)(first / p.piece), all = p.pieces * p.E;
+    count(p, (unsigned)((int64_t)mine * p.piece * p.k), i_first, i_first, &twice, &twice);
+    constexpr int DEEP = 8;
+    for (int i = tid; i < all; i += DEEP * THREADS) {
+      int n[DEEP];
+#pragma unroll
+      for (int q = 0; q < DEEP; ++q) n[q] = p.counts[min(i + q * THREADS, all - 1)];
+#pragma unroll
+      for (int q = 0; q < DEEP; ++q)
+        if (i + q * THREADS < all) {
+          const int c = (i + q * THREADS) / p.E, e = i + q * THREADS - c * p.E;
+          atomicAdd(&(c < mine ? before : rest).n[tid & (COPIES - 1)][e], n[q]);
+        }
     }
   } else {
-    count(p, 0, (unsigned)(first * p.k), &before);
-    count(p, (unsigned)(first * p.k), (unsigned)(p.T * p.k), &rest);
+    count(p, 0, i_first, i_all, &before, &rest);
   }
   __syncthreads();
   if (tid < 64) {                            // rows of the experts in front, and of this one in front of the workgroup's
-    const int b = tid < p.E ? total(before, tid) : 0, n = tid < p.E ? b + total(rest, tid) : 0;
+    const bool one = tid < p.E;
+    const int b = one ? total(before, tid) : 0, n = one ? b + total(rest, tid) : 0, again = one ? total(twice, tid) : 0;
     int upto = n;
 #pragma unroll
     for (int d = 1; d < MAX_E; d <<= 1) {
       const int from = __shfl_up(upto, d);
       if (lane >= d) upto += from;
     }
-    if (tid < MAX_E) next[tid] = upto - n + b;
-    if (blockIdx.x == 0 && tid < p.E) {
+    if (tid < MAX_E) next[tid] = upto - n + b + again;
+    if (blockIdx.x == 0 && one) {
       p.offsets[tid + 1] = upto;
       if (tid == 0) p.offsets[0] = 0;
     }
   }
-  const int batch = THREADS / p.k;           // tokens whose slots are worked out at once, one to a thread
   for (int64_t t0 = first; t0 < last; t0 += batch) {
-    const int tokens = (int)min((int64_t)batch, last - t0), n = tokens * p.k;
-    for (int i = tid; i < WAVES * MAX_E; i += THREADS) (&of_wave[0][0])[i] = 0;
+    const int tokens = (int)min((int64_t)batch, last - t0), n = tokens * p.k, items = (tokens + side - 1) / side * parts;
+    const unsigned i0 = (unsigned)(t0 * p.k);
+    if (t0 > first) {
+      ids.request(p, i0 + tid, i0 + n);
+      bring(t0, tokens, wave, piece);
+    }
+    if (tid < WAVES * MAX_E) (&of_wave[0][0])[tid] = 0;
     __syncthreads();                         // (`next` is there too)
-    const int e = tid < n ? expert_at(p, (unsigned)(t0 * p.k) + tid) : -1;
+    const int e = ids.at(p, 0, i0 + tid, i0 + n);
     int rank = 0;                            // among the wavefront's slots of the same expert
     for (unsigned long long left = __ballot(e >= 0); left;) {
       const int of = __builtin_amdgcn_readlane(e, __ffsll((long long)left) - 1);
@@ -154,37 +194,28 @@ __global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p) 
       for (int w = 0; w < WAVES - 1; ++w) slot += w < wave ? of_wave[w][e] : 0;
     }
     slots[tid] = slot;
-    if (tid < n) p.slot_of[t0 * p.k + tid] = slot;
+    if (tid < n) p.slot_of[(int64_t)i0 + tid] = slot;
     __syncthreads();
     if (tid < MAX_E)
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) next[tid] += of_wave[w][tid];
-    // The rows: a wavefront takes COPY times 64 chunks of a token's row at a time, of short rows several tokens'.
-    int shift = 6;                           // lanes to a row: a power of two
-    while (shift > 0 && p.chunks <= 1 << (shift - 1)) --shift;
-    const int side = 64 >> shift, column = lane & ((1 << shift) - 1);
-    const int parts = (p.chunks + (COPY << shift) - 1) / (COPY << shift);
-    for (int item = wave; item < ((tokens + side - 1) / side) * parts; item += WAVES) {
-      const int group = item / parts, part = item - group * parts;
-      const int token = group * side + (lane >> shift), c0 = part * (COPY << shift) + column;
-      if (token >= tokens) continue;
-      const u32x4* const from = (const u32x4*)p.x + (t0 + token) * p.chunks + c0;
-      u32x4 v[COPY];
-#pragma unroll
-      for (int q = 0; q < COPY; ++q)
-        if (c0 + (q << shift) < p.chunks) v[q] = from[q << shift];
+    for (int item = wave; item < items; item += WAVES) {
+      const Piece now = piece;
+      if (item + WAVES < items) bring(t0, tokens, item + WAVES, piece);
+      if (now.token >= tokens) continue;
       for (int j = 0; j < p.k; ++j) {
-        const int to = slots[token * p.k + j];
+        const int to = slots[now.token * p.k + j];
         if (to < 0) continue;
-        u32x4* const at = (u32x4*)p.rows + (int64_t)to * p.chunks + c0;
+        u32x4* const at = (u32x4*)p.rows + (int64_t)to * p.chunks + now.c0;
 #pragma unroll
         for (int q = 0; q < COPY; ++q)
-          if (c0 + (q << shift) < p.chunks) at[q << shift] = v[q];
+          if (now.c0 + (q << shift) < p.chunks) at[q << shift] = now.v[q];
       }
     }
     __syncthreads();                         // (`slots`, `next` and `of_wave` begin anew)
   }
 }
+static_assert(WAVES * MAX_E <= THREADS, "of_wave is cleared at once");
 
 // ---- combine ---------------------------------------------------------------------------------------
 // Elements of a chunk: 4 fp32 or 8 bf16.
@@ -435,7 +466,7 @@ int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used
     MOEP_HIP(hipGetLastError());
   }
   Timed timed("dispatch_rows", s);
-  hipLaunchKernelGGL(dispatch_rows_kernel, dim3((unsigned)(T > 0 ? ceil_div(T, plan.per) : 1)), dim3(THREADS), 0, s, p);
+  hipLaunchKernelGGL(dispatch_rows_kernel, dim3((unsigned)(T > 0 ? ceil_div(T, plan.per) : 1)), dim3(THREADS), 0, s, p, row_shift(p.chunks));
   MOEP_HIP(hipGetLastError());
   return MOEP_OK;
 }
