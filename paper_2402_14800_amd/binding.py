@@ -8,6 +8,7 @@ fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from typing import Dict, Optional, Tuple
@@ -616,6 +617,10 @@ def _call_on(dev: torch.device, call, *args) -> None:
             _check(call(*args, _raw_stream(dev.index)))
 
 
+def _given(*tensors):
+    return [t for t in tensors if t is not None]
+
+
 def _slot_rows(rows, slot_of, what: str):
     """T, k, H, R and the type code of rows [R,H] named by slot_of [T,k]."""
     if rows.dim() != 2 or slot_of.dim() != 2 or slot_of.dtype != torch.int32:
@@ -628,6 +633,7 @@ def _slot_weights(weights, slot_of, what: str):
         raise ValueError(f"{what}: weights must be [T, k] in float32, as slot_of is")
 
 
+@functools.lru_cache(maxsize=256)
 def moe_dispatch_rows_workspace(T: int, k: int, E: int) -> int:
     return int(_lib.moe_dispatch_rows_workspace(T, k, E))
 
@@ -645,12 +651,12 @@ def moe_dispatch_rows(x, experts, num_experts: int, used=None, rows=None, worksp
         raise ValueError("moe_dispatch_rows: used must be [T] in int32")
     if rows is not None and (rows.shape != (T * k, H) or rows.dtype != x.dtype):
         raise ValueError("moe_dispatch_rows: rows must be [T * k, H], of x's type")
-    dev = _dev(*(t for t in (x, experts, used, rows) if t is not None))
+    dev = _dev(x, experts, *_given(used, rows))
     if rows is None:
         rows = _empty(T * k, H, dtype=x.dtype, device=dev)
-    slot_of = _empty(T, k, dtype=torch.int32, device=dev)
+    slot_of = torch.empty_like(experts)
     offsets = _empty(max(num_experts, 0) + 1, dtype=torch.int32, device=dev)
-    need = _lib.moe_dispatch_rows_workspace(T, k, num_experts)
+    need = moe_dispatch_rows_workspace(T, k, num_experts)
     ws = _workspace(need, dev, workspace) if need or workspace is not None else None
     _call_on(dev, _lib.moe_dispatch_rows, _ptr(x), _ptr(experts), _ptr(used), T, k, num_experts, H, dt, _ptr(rows), _ptr(slot_of),
              _ptr(offsets), _ptr(ws), ws.numel() if ws is not None else 0)
@@ -683,7 +689,7 @@ def moe_combine_rows_backward(dout, y, slot_of, weights=None, weight_gradient: b
     _slot_weights(weights, slot_of, "moe_combine_rows_backward")
     if dout.shape != (T, H) or dout.dtype != y.dtype or (dy is not None and (dy.shape != y.shape or dy.dtype != y.dtype)):
         raise ValueError("moe_combine_rows_backward: dout must be [T, H] and dy like y, of y's type")
-    dev = _dev(*(t for t in (y, dout, slot_of, weights, dy) if t is not None))
+    dev = _dev(y, dout, slot_of, *_given(weights, dy))
     if dy is None:
         dy = _empty(R, H, dtype=y.dtype, device=dev)
     dweights = _empty(T, k, dtype=torch.float32, device=dev) if weight_gradient else None

@@ -32,6 +32,7 @@ struct AnswerArgs {
   void* grad; int64_t ld_grad;
   int64_t stream_rows;                       // the launch's first rows are read past the caches: so many of them
   bool stream_grad;                          // and the gradient is written past them
+  int parts, span;                           // GRADIENT: workgroups to a row, and chunks to each of them
 };
 
 // exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, 1e-9 of the sum.)
@@ -185,24 +186,25 @@ __device__ __forceinline__ Stats add_row(const Row<S>& row, int tid, float c, bo
 
 // HELD: the row fits the workgroup's registers (LOSS_AND_GRADIENT, the one mode that uses a row twice).
 template <typename S, int B, int MODE, bool HELD>
-__global__ __launch_bounds__(B, MODE == LOSS ? 7 : 1) void answers_kernel(AnswerArgs p) {
+__global__ __launch_bounds__(B, MODE != LOSS_AND_GRADIENT ? 7 : 1) void answers_kernel(AnswerArgs p) {
   constexpr int N = Elements<S>::N;
   __shared__ float shared[3 * (B / 64)];
   int tid = threadIdx.x;
   // (the gradient by itself: the rows that the loss read last are the ones that the caches still hold)
-  const int64_t t = MODE == GRADIENT ? p.T - 1 - blockIdx.x : blockIdx.x;
+  const int64_t t = MODE == GRADIENT ? p.T - 1 - blockIdx.x / (unsigned)p.parts : blockIdx.x;
   const bool stream = MODE != GRADIENT && t < p.stream_rows, stream_grad = MODE == GRADIENT || p.stream_grad;
   const Row<S> row(p.logits, p.ld, p.V, t, p.T);
-  const int tiles = HELD ? 1 : (row.chunks + B * NC - 1) / (B * NC);
   S* const out = MODE == LOSS ? nullptr : (S*)p.grad + t * p.ld_grad;
   const bool aligned = (((uintptr_t)out ^ (uintptr_t)row.at) & 15) == 0;
+  const int c_first = MODE == GRADIENT ? (int)(blockIdx.x % (unsigned)p.parts) * p.span : 0;
+  const int c_end = MODE == GRADIENT ? min(row.chunks, c_first + p.span) : row.chunks;
   auto write_zeros = [&]() {
-    for (int k = tid; k < row.chunks; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0}, stream_grad);
+    for (int k = c_first + tid; k < c_end; k += B) store_chunk(row, out, aligned, k, u32x4{0, 0, 0, 0}, stream_grad);
   };
   const int64_t y = p.tokens[t];
   const float c = uniform(LOG2E / p.tau);
   float m, scale, factor, shift = 0.f;                       // the gradient is scale [i = y] - factor exp2((z - m) c + shift)
-  u32x4 v[NC];
+  u32x4 v[HELD ? NC : 1];
   if (MODE != GRADIENT) {
     bool left_out = y < 0;
     if (p.offsets) left_out = left_out || p.first + t < p.offsets[0] || p.first + t >= p.offsets[2 * p.pairs];
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(B, MODE == LOSS ? 7 : 1) void answers_kernel(Answer
       if (p.ref) ref = p.ref[t];
     }
     Stats all = {NEG_INF, 0.f, 0.f};
-    if (!HELD) {
+    if constexpr (!HELD) {
       all = add_row<S, B>(row, tid, c, stream);
     } else {
       if (stream) {
@@ -278,29 +280,33 @@ __global__ __launch_bounds__(B, MODE == LOSS ? 7 : 1) void answers_kernel(Answer
     factor = scale;
   }
   const int at_y = y < p.V ? (int)((y + row.lead) / N) : -1, of_y = y < p.V ? (int)((y + row.lead) % N) : 0;
-  for (int i = 0; i < tiles; ++i) {
-    tid = thread_again(tid);
-    if (!HELD || MODE == GRADIENT) {
-      request_tile<S, B>(row, i, tid, v);
-      cut_ends<S, B>(row, i, tid, v);
-    } else {
-      use_again(v);
+  auto write = [&](const u32x4& z, int at) {
+    if (at >= c_end) return;
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float d = Elements<S>::get(z, j) - m;
+      x[j] = -factor * exp2_fast(MODE == GRADIENT ? fmaf(d, c, shift) : d * c);
     }
+    if (at == at_y)
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const int at = i * (B * NC) + n * B + tid;
-      if (at < row.chunks) {
-        float x[N];
+      for (int j = 0; j < N; ++j) x[j] += j == of_y ? scale : 0.f;
+    store_chunk(row, out, aligned, at, Elements<S>::pack(x), stream_grad);
+  };
+  if constexpr (HELD) {
+    tid = thread_again(tid);
+    use_again(v);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float d = Elements<S>::get(v[n], j) - m;
-          x[j] = -factor * exp2_fast(MODE == GRADIENT ? fmaf(d, c, shift) : d * c);
-        }
-        if (at == at_y)
-#pragma unroll
-          for (int j = 0; j < N; ++j) x[j] += j == of_y ? scale : 0.f;
-        store_chunk(row, out, aligned, at, Elements<S>::pack(x), stream_grad);
-      }
+    for (int n = 0; n < NC; ++n) write(v[n], n * B + tid);
+  } else {
+    const int first = c_first / (GROUP * B), end = (c_end + GROUP * B - 1) / (GROUP * B);
+    Group now, then;
+    request_group<S, B>(row, first, tid, false, now);
+    for (int g = first; g < end; ++g) {
+      if (g + 1 < end) request_group<S, B>(row, g + 1, tid, false, then);
+      cut_group<S, B>(row, g, tid, now);
+      now.each([&](u32x4& x, int n) { write(x, (g * GROUP + n) * B + tid); });
+      now = then;
     }
   }
 }
@@ -371,11 +377,33 @@ __global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
   }
 }
 
+// Threads per row where it is not held.  us, 64 / 256 / 512 threads.  The loss alone: 1 row of 32000 bf16 - / 7.9 / 7.5; 128 of 131072 - / 18.3 / 14.6; 300 of
+// 50001 - / 14.9 / 15.5; 700 of 32000 - / 14.0 / 16.0; 1001 of 50001 - / 24.1 / 26.3.  The gradient alone: 5000 of 4000 16.5 / 18.3 / 22.5; 3256 of 32000 - / 75.5 /
+// 72.1; 8192 of 32000 - / 198 / 195.
+int threads_to_walk(int64_t T, int64_t chunks, bool gradient) {
+  if (chunks <= 64 * GROUP * 4 && T > 2048) return 64;
+  if (gradient) return chunks <= 512 * GROUP ? 256 : 512;
+  return T >= 256 || chunks <= 256 * GROUP ? 256 : 512;
+}
+// Workgroups to a row of a gradient alone, of `turns` groups of chunks: as many as fill the chip where rows are few.  us, one / so many: 1 row of
+// 262144 bf16 28 / 6.2, 20 31 / 8.1, 128 of 131072 19.5 / 13.6, 300 of 50001 16.3 / 14.5 (6.1 of each the time of an empty launch as measured here).
+int64_t row_parts(int64_t T, int64_t turns) {
+  const int64_t parts = 1024 / T;
+  return parts < 1 ? 1 : parts < turns ? parts : turns;
+}
+// The caches (256 MB behind the XCDs') and what passes them by.  A gradient that comes by itself is written past them, so that they keep the logits that
+// it has yet to read, and its lines need not be written back while the next call reads; the loss alone reads past them what they could not
+// keep for the gradient.  us, without the two / with the first / with both, loss and gradient of pairs: 500 rows of 131072 bf16 92 / 75 / 75,
+// 3256 of 32000 135 / 120 / 115, 8192 of 32000 311 / 292 / 290; keeping 100 MB instead of 160: 82, 119, 290.  Loss and gradient in one read: the logits are not
+// read again, so those of a large batch come past the caches, and the gradient goes past them if it is more than they hold: 3256 of
+// 32000 83 / 71, 4096 of 32000 101 / 88, 8192 of 32000 191 / 180 (the logits alone past them 193), 1001 of 50001 (100 MB) the same.
 constexpr double CACHE_BYTES = 268e6, STREAM_BYTES = 134e6, KEPT_BYTES = 160e6;
 template <int MODE>
 int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
   const int64_t chunks = most_chunks(whole.logits, whole.ld, whole.V, dt);
-  const int threads = MODE == LOSS ? threads_to_read(T, chunks) : threads_to_hold(T, chunks);
+  const int threads = MODE == LOSS_AND_GRADIENT ? threads_to_hold(T, chunks) : threads_to_walk(T, chunks, MODE == GRADIENT);
+  const int64_t turns = threads ? ceil_div(chunks, (int64_t)GROUP * threads) : 1;
+  const int64_t parts = MODE == GRADIENT ? row_parts(T, turns) : 1;
   const double bytes = (double)whole.V * (double)dtype_size(dt);       // of a row
   // rows of the loss alone in front of those that the caches can keep for the gradient; all of a large batch whose gradient comes with it
   const int64_t streamed = MODE == LOSS ? T - (int64_t)(KEPT_BYTES / bytes) : bytes * (double)T > STREAM_BYTES ? T : 0;
@@ -388,6 +416,9 @@ int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_
     p.first = t;
     p.stream_rows = streamed - t;
     p.stream_grad = bytes * (double)T > CACHE_BYTES;
+    p.parts = (int)parts;
+    p.span = (int)(ceil_div(turns, parts) * GROUP * threads);
+    const unsigned blocks = (unsigned)(p.T * parts);
     const int64_t size = (int64_t)dtype_size(dt);
     p.logits = (const char*)whole.logits + t * whole.ld * size;
     p.tokens += t;
@@ -402,10 +433,10 @@ int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_
     auto with = [&](auto b, auto held) {
       constexpr int B = decltype(b)::value;
       constexpr bool HELD = decltype(held)::value && MODE == LOSS_AND_GRADIENT;
-      if (dt == MOEP_BF16) hipLaunchKernelGGL((answers_kernel<uint16_t, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
-      else hipLaunchKernelGGL((answers_kernel<float, B, MODE, HELD>), dim3((unsigned)p.T), dim3(B), 0, s, p);
+      if (dt == MOEP_BF16) hipLaunchKernelGGL((answers_kernel<uint16_t, B, MODE, HELD>), dim3(blocks), dim3(B), 0, s, p);
+      else hipLaunchKernelGGL((answers_kernel<float, B, MODE, HELD>), dim3(blocks), dim3(B), 0, s, p);
     };
-    if constexpr (MODE == LOSS) {
+    if constexpr (MODE != LOSS_AND_GRADIENT) {
       if (threads == 64) with(std::integral_constant<int, 64>{}, std::false_type{});
       else if (threads == 256) with(std::integral_constant<int, 256>{}, std::false_type{});
       else with(std::integral_constant<int, 512>{}, std::false_type{});

@@ -154,8 +154,8 @@ def test_binding_refuses_before_it_calls(bad):
 def test_kernels_do_not_spill():
     usage = build.kernel_resource_usage("answers.hip")
     rows = {n: u for n, u in usage.items() if "answers_kernel" in n}
-    # 2 types: the loss alone by 3 workgroup sizes, loss and gradient by 5 and not held, the gradient by 5
-    assert len(rows) == 28
+    # 2 types: the loss alone and the gradient alone by 3 workgroup sizes, both together by 5 and not held
+    assert len(rows) == 24
     for name, u in rows.items():
         assert u["ScratchSize"] == 0 and u["VGPRs Spill"] == 0 and u["Occupancy"] >= 4, (name, u)
     for name, u in build.kernel_resource_usage("rows.hip").items():
