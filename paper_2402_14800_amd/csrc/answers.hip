@@ -397,7 +397,7 @@ int64_t row_parts(int64_t T, int64_t turns) {
 // 3256 of 32000 135 / 120 / 115, 8192 of 32000 311 / 292 / 290; keeping 100 MB instead of 160: 82, 119, 290.  Loss and gradient in one read: the logits are not
 // read again, so those of a large batch come past the caches, and the gradient goes past them if it is more than they hold: 3256 of
 // 32000 83 / 71, 4096 of 32000 101 / 88, 8192 of 32000 191 / 180 (the logits alone past them 193), 1001 of 50001 (100 MB) the same.
-constexpr double CACHE_BYTES = 268e6, STREAM_BYTES = 134e6, KEPT_BYTES = 160e6;
+constexpr double HELD_BYTES = 268.5e6, LARGE_BYTES = 134e6, KEPT_BYTES = 160e6;
 template <int MODE>
 int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_t s, const char* name) {
   const int64_t chunks = most_chunks(whole.logits, whole.ld, whole.V, dt);
@@ -406,7 +406,7 @@ int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_
   const int64_t parts = MODE == GRADIENT ? row_parts(T, turns) : 1;
   const double bytes = (double)whole.V * (double)dtype_size(dt);       // of a row
   // rows of the loss alone in front of those that the caches can keep for the gradient; all of a large batch whose gradient comes with it
-  const int64_t streamed = MODE == LOSS ? T - (int64_t)(KEPT_BYTES / bytes) : bytes * (double)T > STREAM_BYTES ? T : 0;
+  const int64_t streamed = MODE == LOSS ? T - (int64_t)(KEPT_BYTES / bytes) : bytes * (double)T > LARGE_BYTES ? T : 0;
   Timed timed(name, s);
   const int64_t launches = ceil_div(T, LAUNCH_ROWS);
   for (int64_t i = 0; i < launches; ++i) {
@@ -415,7 +415,7 @@ int launch_answers(const AnswerArgs& whole, int64_t T, moep_dtype dt, hipStream_
     p.T = T - t < LAUNCH_ROWS ? T - t : LAUNCH_ROWS;
     p.first = t;
     p.stream_rows = streamed - t;
-    p.stream_grad = bytes * (double)T > CACHE_BYTES;
+    p.stream_grad = bytes * (double)T > HELD_BYTES;
     p.parts = (int)parts;
     p.span = (int)(ceil_div(turns, parts) * GROUP * threads);
     const unsigned blocks = (unsigned)(p.T * parts);

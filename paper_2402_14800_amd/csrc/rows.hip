@@ -19,6 +19,13 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int MAX_E = 32, MAX_K = 16;
 
+// STREAM: past the caches.
+template <bool STREAM> __device__ __forceinline__ u32x4 load(const u32x4* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }
+template <bool STREAM> __device__ __forceinline__ void store(u32x4* p, const u32x4& v) {
+  if (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
 // ---- dispatch --------------------------------------------------------------------------------------
 struct DispatchArgs {
   const char* x;
@@ -26,30 +33,36 @@ struct DispatchArgs {
   const int32_t* used;                       // [T], may be NULL: all k
   int64_t T;
   int k, E, chunks;                          // chunks of 16 bytes to a row
-  int per;                                   // tokens of a workgroup
-  int32_t* counts;                           // [pieces, E] ids of each expert in pieces of `piece` tokens; NULL: not counted ahead
-  int64_t piece;
-  int pieces;
+  int32_t* counts;                           // [pieces, E]: ids of each expert in pieces of `piece` tokens; NULL: not counted ahead
+  int piece, pieces;
   char* rows;
   int32_t* slot_of;                          // [T, k]
   int32_t* offsets;                          // [E + 1]
 };
 
-// Slots i, i + THREADS, .. as they are in memory (beyond `end` slot end - 1 again: all loads at once, and no lane's waits for another's),
+// Slots i, i + B, .. as they are in memory (beyond `end` slot end - 1 again: all loads at once, and no lane's waits for another's),
 // and the expert of each: -1 if the slot is not used, or beyond the end.
-template <int DEEP>
+template <int DEEP, int B>
 struct Ids {
-  int expert[DEEP], used[DEEP];
+  int expert[DEEP], used[DEEP], j[DEEP];
   __device__ __forceinline__ void request(const DispatchArgs& p, unsigned i, unsigned end) {
 #pragma unroll
-    for (int q = 0; q < DEEP; ++q) expert[q] = p.experts[min(i + q * THREADS, end - 1)];
-    if (p.used)
+    for (int q = 0; q < DEEP; ++q) expert[q] = p.experts[min(i + q * B, end - 1)];
+    if (!p.used) return;
+    const unsigned k = (unsigned)p.k, last = (end - 1) / k, t_step = B / k, j_step = B - t_step * k;
+    unsigned t = i / k, slot = i - t * k;    // (of the next ones without a division)
 #pragma unroll
-      for (int q = 0; q < DEEP; ++q) used[q] = p.used[min(i + q * THREADS, end - 1) / (unsigned)p.k];
+    for (int q = 0; q < DEEP; ++q) {
+      j[q] = (int)slot;
+      used[q] = p.used[min(t, last)];
+      t += t_step;
+      slot += j_step;
+      if (slot >= k) { slot -= k; ++t; }
+    }
   }
   __device__ __forceinline__ int at(const DispatchArgs& p, int q, unsigned i, unsigned end) const {
-    bool there = i + q * THREADS < end && (unsigned)expert[q] < (unsigned)p.E;
-    if (p.used) there = there && (int)((i + q * THREADS) % (unsigned)p.k) < used[q];
+    bool there = i + q * B < end && (unsigned)expert[q] < (unsigned)p.E;
+    if (p.used) there = there && j[q] < used[q];
     return there ? expert[q] : -1;
   }
 };
@@ -69,9 +82,9 @@ __device__ __forceinline__ int total(const Counts& c, int e) {
 // Adds the ids of slots i0 .. i1 - 1, those in front of `split` to `a`, the others to `b`.
 __device__ __forceinline__ void count(const DispatchArgs& p, unsigned i0, unsigned split, unsigned i1, Counts* a, Counts* b) {
   const int copy = threadIdx.x & (COPIES - 1);
-  constexpr int DEEP = 16;
+  constexpr int DEEP = 8;
   for (unsigned i = i0 + threadIdx.x; i < i1; i += DEEP * THREADS) {
-    Ids<DEEP> ids;
+    Ids<DEEP, THREADS> ids;
     ids.request(p, i, i1);
 #pragma unroll
     for (int q = 0; q < DEEP; ++q) {
@@ -91,101 +104,128 @@ __global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
   if ((int)threadIdx.x < p.E) p.counts[(int64_t)blockIdx.x * p.E + threadIdx.x] = total(c, threadIdx.x);
 }
 
-// The rows: a wavefront takes COPY times 64 chunks of a token's row at a time, of short rows several tokens'.
-constexpr int COPY = 4;
-struct Piece {
-  u32x4 v[COPY];
-  int token, c0;
-};
+// Among the wavefront's slots of the same expert e (-1: none) how many come before this lane's; and how many there are, to of_wave[e].
+__device__ __forceinline__ int rank_in_wave(int e, int* of_wave) {
+  int rank = 0;
+  for (unsigned long long left = __ballot(e >= 0); left;) {
+    const int of = __builtin_amdgcn_readlane(e, __ffsll((long long)left) - 1);
+    const unsigned long long same = __ballot(e == of);
+    if (e == of) {
+      rank = __builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0u));
+      of_wave[e] = __popcll(same);
+    }
+    left &= ~same;
+  }
+  return rank;
+}
+// Sum of the lanes' numbers up to and with this one, over the first 32 lanes.
+__device__ __forceinline__ int running_sum(int n, int lane) {
+#pragma unroll
+  for (int d = 1; d < MAX_E; d <<= 1) {
+    const int from = __shfl_up(n, d);
+    if (lane >= d) n += from;
+  }
+  return n;
+}
+__device__ __forceinline__ void write_offsets(const DispatchArgs& p, int e, int upto) {
+  if (blockIdx.x != 0 || e >= p.E) return;
+  p.offsets[e + 1] = upto;
+  if (e == 0) p.offsets[0] = 0;
+}
 
-__global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p, int shift) {
-  __shared__ Counts before, rest, twice;
+// Up to B slots: every workgroup works them all out, one to a thread, and copies one token's row.
+template <int B>
+__global__ __launch_bounds__(B) void dispatch_few_rows_kernel(DispatchArgs p) {
+  constexpr int W = B / 64;
+  __shared__ int next[MAX_E];
+  __shared__ int of_wave[W][MAX_E];
+  __shared__ int slots[B];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int t = (int)blockIdx.x, n = (int)p.T * p.k;
+  const u32x4* const from = (const u32x4*)p.x + (int64_t)t * p.chunks;
+  Ids<1, B> ids;
+  u32x4 v = {0, 0, 0, 0};                    // (the row's first chunks are asked for with the ids)
+  if (n > 0) {
+    ids.request(p, tid, n);
+    if (tid < p.chunks) v = from[tid];
+  }
+  for (int i = tid; i < W * MAX_E; i += B) (&of_wave[0][0])[i] = 0;
+  __syncthreads();
+  const int e = n > 0 ? ids.at(p, 0, tid, n) : -1;
+  const int rank = rank_in_wave(e, of_wave[wave]);
+  __syncthreads();
+  if (tid < 64) {                            // rows in front of each wavefront's, of its expert and of those before
+    int all = 0;
+    if (tid < MAX_E)
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const int m = of_wave[w][tid];
+        of_wave[w][tid] = all;
+        all += m;
+      }
+    const int upto = running_sum(all, lane);
+    if (tid < MAX_E) next[tid] = upto - all;
+    write_offsets(p, tid, upto);
+  }
+  __syncthreads();
+  const int slot = e >= 0 ? next[e] + of_wave[wave][e] + rank : -1;
+  slots[tid] = slot;
+  if (blockIdx.x == 0 && tid < n) p.slot_of[tid] = slot;
+  if (n == 0) return;
+  __syncthreads();
+  for (int c = tid; c < p.chunks; c += B) {
+    if (c >= B) v = from[c];
+    for (int j = 0; j < p.k; ++j) {
+      const int to = slots[t * p.k + j];
+      if (to >= 0) ((u32x4*)p.rows)[(int64_t)to * p.chunks + c] = v;
+    }
+  }
+}
+
+// The slots' numbers, a piece of the tokens to a workgroup.
+__global__ __launch_bounds__(THREADS) void place_rows_kernel(DispatchArgs p) {
+  __shared__ Counts before, rest;
   __shared__ int next[MAX_E];                // the number of the next row of each expert
   __shared__ int of_wave[WAVES][MAX_E];
-  __shared__ int slots[THREADS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t first = (int64_t)blockIdx.x * p.per, last = min(p.T, first + p.per);
-  const unsigned i_first = (unsigned)(first * p.k), i_all = (unsigned)(p.T * p.k);
-  // (2^shift lanes to a row)
-  const int side = 64 >> shift, parts = (p.chunks + (COPY << shift) - 1) / (COPY << shift);
-  const int batch = THREADS / p.k;           // tokens whose slots are worked out at once, one to a thread
-  auto bring = [&](int64_t t0, int tokens, int item, Piece& x) {
-    const int group = item / parts;
-    x.token = group * side + (lane >> shift);
-    x.c0 = (item - group * parts) * (COPY << shift) + (lane & ((1 << shift) - 1));
-    const u32x4* const from = (const u32x4*)p.x + (t0 + x.token) * p.chunks + x.c0;
-#pragma unroll
-    for (int q = 0; q < COPY; ++q)
-      if (x.token < tokens && x.c0 + (q << shift) < p.chunks) x.v[q] = from[q << shift];
-  };
-  // (what the first batch needs is asked for before the counting, which takes longer than it)
-  Ids<1> ids;
-  Piece piece;
-  if (first < last) {
-    const int tokens = (int)min((int64_t)batch, last - first);
-    ids.request(p, i_first + tid, i_first + tokens * p.k);
-    bring(first, tokens, wave, piece);
-  }
+  const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
+  const unsigned i0 = (unsigned)(t0 * p.k), i1 = (unsigned)(t1 * p.k), all = (unsigned)(p.T * p.k);
+  Ids<1, THREADS> ids;                       // (asked for before the counting, which takes longer than they do)
+  ids.request(p, i0 + tid, i1);
   clear(&before);
   clear(&rest);
-  clear(&twice);
   __syncthreads();
   if (p.counts) {
-    // pieces in front of the workgroup's (its tokens lie in one), and all others; of its own the ids in front of the workgroup's, which
-    // are counted among the others as well
-    const int mine = (int)(first / p.piece), all = p.pieces * p.E;
-    count(p, (unsigned)((int64_t)mine * p.piece * p.k), i_first, i_first, &twice, &twice);
+    const unsigned mine = blockIdx.x * (unsigned)p.E, n = (unsigned)p.pieces * (unsigned)p.E, e_step = THREADS % (unsigned)p.E;
     constexpr int DEEP = 8;
-    for (int i = tid; i < all; i += DEEP * THREADS) {
-      int n[DEEP];
+    unsigned e = tid % (unsigned)p.E;
+    for (unsigned i = tid; i < n; i += DEEP * THREADS) {
+      int c[DEEP];
 #pragma unroll
-      for (int q = 0; q < DEEP; ++q) n[q] = p.counts[min(i + q * THREADS, all - 1)];
+      for (int q = 0; q < DEEP; ++q) c[q] = p.counts[min(i + q * THREADS, n - 1)];
 #pragma unroll
-      for (int q = 0; q < DEEP; ++q)
-        if (i + q * THREADS < all) {
-          const int c = (i + q * THREADS) / p.E, e = i + q * THREADS - c * p.E;
-          atomicAdd(&(c < mine ? before : rest).n[tid & (COPIES - 1)][e], n[q]);
-        }
+      for (int q = 0; q < DEEP; ++q) {
+        if (i + q * THREADS < n) atomicAdd(&(i + q * THREADS < mine ? before : rest).n[(tid >> 3) & (COPIES - 1)][e], c[q]);
+        e += e_step;
+        if (e >= (unsigned)p.E) e -= p.E;
+      }
     }
   } else {
-    count(p, 0, i_first, i_all, &before, &rest);
+    count(p, 0, i0, all, &before, &rest);
   }
   __syncthreads();
   if (tid < 64) {                            // rows of the experts in front, and of this one in front of the workgroup's
-    const bool one = tid < p.E;
-    const int b = one ? total(before, tid) : 0, n = one ? b + total(rest, tid) : 0, again = one ? total(twice, tid) : 0;
-    int upto = n;
-#pragma unroll
-    for (int d = 1; d < MAX_E; d <<= 1) {
-      const int from = __shfl_up(upto, d);
-      if (lane >= d) upto += from;
-    }
-    if (tid < MAX_E) next[tid] = upto - n + b + again;
-    if (blockIdx.x == 0 && one) {
-      p.offsets[tid + 1] = upto;
-      if (tid == 0) p.offsets[0] = 0;
-    }
+    const int b = tid < p.E ? total(before, tid) : 0, n = tid < p.E ? b + total(rest, tid) : 0;
+    const int upto = running_sum(n, lane);
+    if (tid < MAX_E) next[tid] = upto - n + b;
+    write_offsets(p, tid, upto);
   }
-  for (int64_t t0 = first; t0 < last; t0 += batch) {
-    const int tokens = (int)min((int64_t)batch, last - t0), n = tokens * p.k, items = (tokens + side - 1) / side * parts;
-    const unsigned i0 = (unsigned)(t0 * p.k);
-    if (t0 > first) {
-      ids.request(p, i0 + tid, i0 + n);
-      bring(t0, tokens, wave, piece);
-    }
+  for (unsigned i = i0; i < i1; i += THREADS) {
+    if (i > i0) ids.request(p, i + tid, i1);
     if (tid < WAVES * MAX_E) (&of_wave[0][0])[tid] = 0;
     __syncthreads();                         // (`next` is there too)
-    const int e = ids.at(p, 0, i0 + tid, i0 + n);
-    int rank = 0;                            // among the wavefront's slots of the same expert
-    for (unsigned long long left = __ballot(e >= 0); left;) {
-      const int of = __builtin_amdgcn_readlane(e, __ffsll((long long)left) - 1);
-      const unsigned long long same = __ballot(e == of);
-      if (e == of) {
-        rank = __builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0u));
-        of_wave[wave][e] = __popcll(same);
-      }
-      left &= ~same;
-    }
+    const int e = ids.at(p, 0, i + tid, i1);
+    const int rank = rank_in_wave(e, of_wave[wave]);
     __syncthreads();
     int slot = -1;
     if (e >= 0) {
@@ -193,29 +233,38 @@ __global__ __launch_bounds__(THREADS) void dispatch_rows_kernel(DispatchArgs p, 
 #pragma unroll
       for (int w = 0; w < WAVES - 1; ++w) slot += w < wave ? of_wave[w][e] : 0;
     }
-    slots[tid] = slot;
-    if (tid < n) p.slot_of[(int64_t)i0 + tid] = slot;
+    if (i + tid < i1) p.slot_of[i + tid] = slot;
     __syncthreads();
     if (tid < MAX_E)
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) next[tid] += of_wave[w][tid];
-    for (int item = wave; item < items; item += WAVES) {
-      const Piece now = piece;
-      if (item + WAVES < items) bring(t0, tokens, item + WAVES, piece);
-      if (now.token >= tokens) continue;
-      for (int j = 0; j < p.k; ++j) {
-        const int to = slots[now.token * p.k + j];
-        if (to < 0) continue;
-        u32x4* const at = (u32x4*)p.rows + (int64_t)to * p.chunks + now.c0;
-#pragma unroll
-        for (int q = 0; q < COPY; ++q)
-          if (now.c0 + (q << shift) < p.chunks) at[q << shift] = now.v[q];
-      }
-    }
-    __syncthreads();                         // (`slots`, `next` and `of_wave` begin anew)
+    __syncthreads();                         // (`next` and `of_wave` begin anew)
   }
 }
 static_assert(WAVES * MAX_E <= THREADS, "of_wave is cleared at once");
+
+// The rows: a thread takes one chunk of a token's row (2^shift lanes to a row) and stores it k times.
+template <int KG, bool STREAM>
+__global__ __launch_bounds__(THREADS) void copy_rows_kernel(DispatchArgs p, int shift) {
+  const int lane = threadIdx.x & 63;
+  const int side = 64 >> shift, parts = (p.chunks + (1 << shift) - 1) >> shift;
+  const int64_t item = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
+  const int64_t group = item / parts;
+  const int64_t t = group * side + (lane >> shift);
+  const int c = (int)(item - group * parts) * (1 << shift) + (lane & ((1 << shift) - 1));
+  if (t >= p.T || c >= p.chunks) return;
+  const u32x4 v = ((const u32x4*)p.x)[t * p.chunks + c];
+  for (int j0 = 0; j0 < p.k; j0 += KG) {
+    int slot[KG];
+#pragma unroll
+    for (int j = 0; j < KG; ++j) slot[j] = j0 + j < p.k ? p.slot_of[t * p.k + j0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < KG; ++j)
+      if (slot[j] >= 0) {
+        store<STREAM>((u32x4*)p.rows + (int64_t)slot[j] * p.chunks + c, v);
+      }
+  }
+}
 
 // ---- combine ---------------------------------------------------------------------------------------
 // Elements of a chunk: 4 fp32 or 8 bf16.
@@ -252,7 +301,7 @@ struct CombineArgs {
 };
 
 // A thread takes one chunk of a token's row, KG slots' at once, so that their loads are in flight together; the sum goes in the slots' order.
-template <typename S, int KG>
+template <typename S, int KG, bool STREAM>
 __global__ __launch_bounds__(THREADS) void combine_rows_kernel(CombineArgs p, int shift) {
   constexpr int N = Chunk<S>::N;
   const int lane = threadIdx.x & 63;
@@ -276,7 +325,9 @@ __global__ __launch_bounds__(THREADS) void combine_rows_kernel(CombineArgs p, in
     }
 #pragma unroll
     for (int j = 0; j < KG; ++j)
-      if ((unsigned)slot[j] < (unsigned)p.R) v[j] = ((const u32x4*)p.y)[(int64_t)slot[j] * p.chunks + c];
+      if ((unsigned)slot[j] < (unsigned)p.R) {
+        v[j] = load<STREAM>((const u32x4*)p.y + (int64_t)slot[j] * p.chunks + c);
+      }
 #pragma unroll
     for (int j = 0; j < KG; ++j)
       if ((unsigned)slot[j] < (unsigned)p.R)
@@ -288,7 +339,7 @@ __global__ __launch_bounds__(THREADS) void combine_rows_kernel(CombineArgs p, in
 
 // dy and dw of a token by 2^shift lanes, or by all of a workgroup of W wavefronts: each goes through its chunks of dout and of the k rows of y,
 // adding up k products in 32 bits, which are then joined in a fixed order.
-template <typename S, int KG, int W>
+template <typename S, int KG, int W, bool STREAM>
 __global__ __launch_bounds__(THREADS) void combine_rows_backward_kernel(CombineArgs p, int shift) {
   constexpr int N = Chunk<S>::N, U = KG > 4 ? 1 : 2;
   __shared__ float joined[WAVES][KG];
@@ -314,11 +365,11 @@ __global__ __launch_bounds__(THREADS) void combine_rows_backward_kernel(CombineA
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (c + u * step < p.chunks) {
-            d[u] = ((const u32x4*)p.dout)[t * p.chunks + c + u * step];
+            d[u] = load<STREAM>((const u32x4*)p.dout + t * p.chunks + c + u * step);
             if (p.dweights)
 #pragma unroll
               for (int j = 0; j < KG; ++j)
-                if (slot[j] >= 0) v[u][j] = ((const u32x4*)p.y)[(int64_t)slot[j] * p.chunks + c + u * step];
+                if (slot[j] >= 0) v[u][j] = load<STREAM>((const u32x4*)p.y + (int64_t)slot[j] * p.chunks + c + u * step);
           }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -333,7 +384,7 @@ __global__ __launch_bounds__(THREADS) void combine_rows_backward_kernel(CombineA
                   if (p.dweights) dot[j] = fmaf(g, Chunk<S>::get(v[u][j], i), dot[j]);
                   x[i] = w[j] * g;
                 }
-                ((u32x4*)p.dy)[(int64_t)slot[j] * p.chunks + c + u * step] = Chunk<S>::pack(x);
+                store<STREAM>((u32x4*)p.dy + (int64_t)slot[j] * p.chunks + c + u * step, Chunk<S>::pack(x));
               }
           }
       }
@@ -378,21 +429,22 @@ int check_4(const char* who, std::initializer_list<const void*> pointers) {
   return MOEP_OK;
 }
 
-// Slots up to which every workgroup counts all ids by itself, in one launch.
-constexpr int64_t ONE_LAUNCH_SLOTS = 8192;
-constexpr int64_t MIN_PIECE = 1024, MAX_PIECES = 512;
-struct DispatchPlan { int64_t piece = 0; int pieces = 0; int per = 1; };
-DispatchPlan plan_dispatch(int64_t T, int k) {
+// What the caches behind the XCDs' hold: where a call reads and writes more, the larger of its streams goes past them.
+constexpr double HELD_BYTES = 268.5e6;
+inline bool past_caches(int64_t rows, int64_t row_bytes) { return (double)rows * (double)row_bytes > HELD_BYTES; }
+// Slots up to which one launch does all of it, and up to which the workgroups that place a piece count all ids by themselves.
+constexpr int FEW_SLOTS = 1024;
+constexpr int64_t COUNT_ALL_SLOTS = 4096;
+constexpr int64_t MOST_COUNTS = 8192;        // that a workgroup adds up
+struct DispatchPlan { int piece = 0, pieces = 0; bool counted = false; };
+DispatchPlan plan_dispatch(int64_t T, int k, int E) {
   DispatchPlan p;
-  if (T * k <= ONE_LAUNCH_SLOTS) {
-    p.per = (int)ceil_div(T, 1024) > 1 ? (int)ceil_div(T, 1024) : 1;
-    return p;
-  }
-  p.per = 16;
-  while (p.per < 1024 && T / p.per > 16384) p.per *= 2;
-  p.piece = ceil_div(ceil_div(T, MAX_PIECES), 1024) * 1024;      // (a multiple of every `per`)
-  if (p.piece < MIN_PIECE) p.piece = MIN_PIECE;
-  p.pieces = (int)ceil_div(T, p.piece);
+  if (T * k <= FEW_SLOTS) return p;
+  p.counted = T * k > COUNT_ALL_SLOTS;
+  int64_t piece = THREADS / k;               // (a slot to a thread)
+  while (p.counted && ceil_div(T, piece) * E > MOST_COUNTS) piece *= 2;
+  p.piece = (int)piece;
+  p.pieces = (int)ceil_div(T, piece);
   return p;
 }
 
@@ -410,26 +462,41 @@ void with_slots(int k, F launch) {
   else launch(std::integral_constant<int, 8>{});
 }
 
-int launch_combine(const CombineArgs& p, moep_dtype dt, hipStream_t s, const char* name) {
-  const int shift = row_shift(p.chunks), side = 64 >> shift;
-  const int64_t parts = ceil_div(p.chunks, 1 << shift), tokens = ((int64_t)1 << 23) / parts * side;   // of a launch
-  Timed timed(name, s);
-  const int64_t row = (int64_t)p.chunks * 16;
-  for (int64_t t = 0; t < p.T; t += tokens) {
-    CombineArgs a = p;
-    a.T = p.T - t < tokens ? p.T - t : tokens;
-    a.slot_of += t * p.k;
-    if (a.weights) a.weights += t * p.k;
-    a.out += t * row;
-    const unsigned blocks = (unsigned)ceil_div(ceil_div(a.T, side) * parts, WAVES);
-    with_slots(p.k, [&](auto kg) {
-      constexpr int KG = decltype(kg)::value;
-      if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_kernel<uint16_t, KG>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
-      else hipLaunchKernelGGL((combine_rows_kernel<float, KG>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
-    });
+// A wavefront to every 64 chunks of a row (of short rows to several): launch(first token, tokens, workgroups, lanes to a row as a power of two),
+// in as many launches as the grids' limit takes.
+template <typename F>
+int in_launches(int64_t T, int chunks, F launch) {
+  const int shift = row_shift(chunks), side = 64 >> shift;
+  const int64_t parts = ceil_div(chunks, 1 << shift), most = (most_workgroups(THREADS) * WAVES / parts - 1) * side;
+  for (int64_t t = 0; t < T; t += most) {
+    const int64_t tokens = T - t < most ? T - t : most;
+    launch(t, tokens, (unsigned)ceil_div(ceil_div(tokens, side) * parts, WAVES), shift);
     MOEP_HIP(hipGetLastError());
   }
   return MOEP_OK;
+}
+
+int launch_combine(const CombineArgs& p, moep_dtype dt, hipStream_t s, const char* name) {
+  Timed timed(name, s);
+  const int64_t row = (int64_t)p.chunks * 16;
+  const bool stream = past_caches(p.R + p.T, row);
+  return in_launches(p.T, p.chunks, [&](int64_t t, int64_t tokens, unsigned blocks, int shift) {
+    CombineArgs a = p;
+    a.T = tokens;
+    a.slot_of += t * p.k;
+    if (a.weights) a.weights += t * p.k;
+    a.out += t * row;
+    with_slots(p.k, [&](auto kg) {
+      constexpr int KG = decltype(kg)::value;
+      auto with = [&](auto streams) {
+        constexpr bool STREAM = decltype(streams)::value;
+        if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_kernel<uint16_t, KG, STREAM>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+        else hipLaunchKernelGGL((combine_rows_kernel<float, KG, STREAM>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+      };
+      if (stream) with(std::true_type{});
+      else with(std::false_type{});
+    });
+  });
 }
 
 }  // namespace
@@ -441,7 +508,8 @@ extern "C" {
 
 size_t moe_dispatch_rows_workspace(int64_t T, int k, int E) {
   if (k < 1 || k > MAX_K || E < 1 || E > MAX_E || T < 0 || T > ((int64_t)1 << 30) / k) return 0;
-  return (size_t)plan_dispatch(T, k).pieces * E * sizeof(int32_t);
+  const DispatchPlan p = plan_dispatch(T, k, E);
+  return p.counted ? (size_t)p.pieces * E * sizeof(int32_t) : 0;
 }
 
 int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used, int64_t T, int k, int E, int H, moep_dtype dt, void* rows,
@@ -457,18 +525,40 @@ int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used
   if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
     return fail(MOEP_EWORKSPACE, "%s: needs a 256-byte aligned workspace of %zu bytes", who, need);
   hipStream_t s = (hipStream_t)hip_stream;
-  const DispatchPlan plan = plan_dispatch(T, k);
-  DispatchArgs p = {(const char*)x, experts, used, T, k, E, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), plan.per,
-                    plan.pieces ? (int32_t*)ws : nullptr, plan.piece, plan.pieces, (char*)rows, slot_of, offsets};
-  if (plan.pieces) {
+  const DispatchPlan plan = plan_dispatch(T, k, E);
+  const int64_t row = (int64_t)H * (int64_t)dtype_size(dt);
+  const DispatchArgs p = {(const char*)x, experts, used, T, k, E, (int)(row / 16), plan.counted ? (int32_t*)ws : nullptr, plan.piece, plan.pieces,
+                          (char*)rows, slot_of, offsets};
+  if (!plan.pieces) {
+    Timed timed("dispatch_rows", s);
+    const dim3 grid((unsigned)(T > 0 ? T : 1));
+    if (T * k <= THREADS) hipLaunchKernelGGL((dispatch_few_rows_kernel<THREADS>), grid, dim3(THREADS), 0, s, p);
+    else hipLaunchKernelGGL((dispatch_few_rows_kernel<FEW_SLOTS>), grid, dim3(FEW_SLOTS), 0, s, p);
+    MOEP_HIP(hipGetLastError());
+    return MOEP_OK;
+  }
+  if (plan.counted) {
     Timed timed("count_rows", s);
     hipLaunchKernelGGL(count_rows_kernel, dim3((unsigned)plan.pieces), dim3(THREADS), 0, s, p);
     MOEP_HIP(hipGetLastError());
   }
-  Timed timed("dispatch_rows", s);
-  hipLaunchKernelGGL(dispatch_rows_kernel, dim3((unsigned)(T > 0 ? ceil_div(T, plan.per) : 1)), dim3(THREADS), 0, s, p, row_shift(p.chunks));
-  MOEP_HIP(hipGetLastError());
-  return MOEP_OK;
+  {
+    Timed timed("place_rows", s);
+    hipLaunchKernelGGL(place_rows_kernel, dim3((unsigned)plan.pieces), dim3(THREADS), 0, s, p);
+    MOEP_HIP(hipGetLastError());
+  }
+  Timed timed("copy_rows", s);
+  return in_launches(T, p.chunks, [&](int64_t t, int64_t tokens, unsigned blocks, int shift) {
+    DispatchArgs a = p;
+    a.T = tokens;
+    a.x += t * row;
+    a.slot_of += t * k;
+    with_slots(k, [&](auto kg) {
+      constexpr int KG = decltype(kg)::value;
+      if (past_caches(T * k + T, row)) hipLaunchKernelGGL((copy_rows_kernel<KG, true>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+      else hipLaunchKernelGGL((copy_rows_kernel<KG, false>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+    });
+  });
 }
 
 int moe_dispatch_rows_backward(const void* drows, const int32_t* slot_of, int64_t T, int k, int H, int64_t R, moep_dtype dt, void* dx,
@@ -511,8 +601,9 @@ int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* sl
   const CombineArgs p = {(const char*)y, slot_of, weights, T, k, (int)((int64_t)H * (int64_t)dtype_size(dt) / 16), (int)R, nullptr, (const char*)dout,
                          (char*)dy, dweights};
   const int shift = row_shift(p.chunks);
-  const bool wide = p.chunks > 64 && T <= 2048;                    // a workgroup to a token
+  const bool wide = p.chunks >= THREADS || (p.chunks > 64 && T <= 2048);   // a workgroup to a token
   const int64_t each = wide ? 1 : (int64_t)WAVES * (64 >> shift), tokens = each << 20;
+  const bool stream = past_caches(2 * R + T, (int64_t)p.chunks * 16);
   Timed timed("combine_rows_backward", s);
   const int64_t row = (int64_t)p.chunks * 16;
   for (int64_t t = 0; t < T; t += tokens) {
@@ -527,8 +618,13 @@ int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* sl
       constexpr int KG = decltype(kg)::value;
       auto with = [&](auto w) {
         constexpr int W = decltype(w)::value;
-        if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_backward_kernel<uint16_t, KG, W>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
-        else hipLaunchKernelGGL((combine_rows_backward_kernel<float, KG, W>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+        auto streaming = [&](auto streams) {
+          constexpr bool STREAM = decltype(streams)::value;
+          if (dt == MOEP_BF16) hipLaunchKernelGGL((combine_rows_backward_kernel<uint16_t, KG, W, STREAM>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+          else hipLaunchKernelGGL((combine_rows_backward_kernel<float, KG, W, STREAM>), dim3(blocks), dim3(THREADS), 0, s, a, shift);
+        };
+        if (stream) streaming(std::true_type{});
+        else streaming(std::false_type{});
       };
       if (wide) with(std::integral_constant<int, WAVES>{});
       else with(std::integral_constant<int, 1>{});
