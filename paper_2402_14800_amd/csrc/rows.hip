@@ -33,7 +33,7 @@ struct DispatchArgs {
   const int32_t* used;                       // [T], may be NULL: all k
   int64_t T;
   int k, E, chunks;                          // chunks of 16 bytes to a row
-  int32_t* counts;                           // [pieces, E]: ids of each expert in pieces of `piece` tokens; NULL: not counted ahead
+  int32_t* counts;                           // [pieces, E]: ids of each expert in pieces of `piece` tokens
   int piece, pieces;
   char* rows;
   int32_t* slot_of;                          // [T, k]
@@ -79,27 +79,22 @@ __device__ __forceinline__ int total(const Counts& c, int e) {
   for (int q = 0; q < COPIES; ++q) n += c.n[q][e];
   return n;
 }
-// Adds the ids of slots i0 .. i1 - 1, those in front of `split` to `a`, the others to `b`.
-__device__ __forceinline__ void count(const DispatchArgs& p, unsigned i0, unsigned split, unsigned i1, Counts* a, Counts* b) {
-  const int copy = threadIdx.x & (COPIES - 1);
-  constexpr int DEEP = 8;
+__global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
+  __shared__ Counts c;
+  clear(&c);
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
+  const unsigned i0 = (unsigned)(t0 * p.k), i1 = (unsigned)(t1 * p.k);
+  constexpr int DEEP = 4;
   for (unsigned i = i0 + threadIdx.x; i < i1; i += DEEP * THREADS) {
     Ids<DEEP, THREADS> ids;
     ids.request(p, i, i1);
 #pragma unroll
     for (int q = 0; q < DEEP; ++q) {
       const int e = ids.at(p, q, i, i1);
-      if (e >= 0) atomicAdd(&(i + q * THREADS < split ? a : b)->n[copy][e], 1);
+      if (e >= 0) atomicAdd(&c.n[threadIdx.x & (COPIES - 1)][e], 1);
     }
   }
-}
-
-__global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
-  __shared__ Counts c;
-  clear(&c);
-  __syncthreads();
-  const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
-  count(p, (unsigned)(t0 * p.k), (unsigned)(t1 * p.k), (unsigned)(t1 * p.k), &c, &c);
   __syncthreads();
   if ((int)threadIdx.x < p.E) p.counts[(int64_t)blockIdx.x * p.E + threadIdx.x] = total(c, threadIdx.x);
 }
@@ -133,10 +128,9 @@ __device__ __forceinline__ void write_offsets(const DispatchArgs& p, int e, int 
   if (e == 0) p.offsets[0] = 0;
 }
 
-// Up to B slots: every workgroup works them all out, one to a thread, and copies one token's row.
-template <int B>
-__global__ __launch_bounds__(B) void dispatch_few_rows_kernel(DispatchArgs p) {
-  constexpr int W = B / 64;
+// Up to THREADS slots: every workgroup works them all out, one to a thread, and copies one token's row.
+__global__ __launch_bounds__(THREADS) void dispatch_few_rows_kernel(DispatchArgs p) {
+  constexpr int B = THREADS, W = WAVES;
   __shared__ int next[MAX_E];
   __shared__ int of_wave[W][MAX_E];
   __shared__ int slots[B];
@@ -182,6 +176,54 @@ __global__ __launch_bounds__(B) void dispatch_few_rows_kernel(DispatchArgs p) {
   }
 }
 
+// Beyond, up to MANY_THREADS x 4 slots: every workgroup counts them all, and places and copies those of `piece` tokens, 64 slots at most.
+constexpr int MANY_THREADS = 1024;
+__global__ __launch_bounds__(MANY_THREADS) void dispatch_many_rows_kernel(DispatchArgs p) {
+  __shared__ Counts before, rest;
+  __shared__ int slots[64];
+  const int tid = threadIdx.x;
+  const int t0 = (int)blockIdx.x * p.piece, tokens = min(p.piece, (int)p.T - t0), n = tokens * p.k;
+  const unsigned i0 = (unsigned)(t0 * p.k), all = (unsigned)((int)p.T * p.k);
+  const int work = tokens * p.chunks;
+  const u32x4* const from = (const u32x4*)p.x + (int64_t)t0 * p.chunks;
+  constexpr int DEEP = 4;
+  Ids<DEEP, MANY_THREADS> ids;
+  Ids<1, 64> own;
+  ids.request(p, tid, all);
+  if (tid < 64) own.request(p, i0 + tid, i0 + n);
+  u32x4 v = {0, 0, 0, 0};                    // (the first chunks of the rows are asked for with the ids)
+  if (tid < work) v = from[tid];
+  for (int i = tid; i < COPIES * (MAX_E + 1); i += MANY_THREADS) { (&before.n[0][0])[i] = 0; (&rest.n[0][0])[i] = 0; }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < DEEP; ++q) {
+    const int e = ids.at(p, q, tid, all);
+    if (e >= 0) atomicAdd(&((unsigned)(tid + q * MANY_THREADS) < i0 ? before : rest).n[tid & (COPIES - 1)][e], 1);
+  }
+  __syncthreads();
+  if (tid < 64) {
+    const int b = tid < p.E ? total(before, tid) : 0, m = tid < p.E ? b + total(rest, tid) : 0;
+    const int upto = running_sum(m, tid);
+    write_offsets(p, tid, upto);
+    const int first = upto - m + b;          // of expert `tid`
+    const int e = own.at(p, 0, i0 + tid, i0 + n);
+    __shared__ int unused[MAX_E];
+    const int rank = rank_in_wave(e, unused);
+    const int slot = __shfl(first, e >= 0 ? e : 0) + rank;
+    slots[tid] = e >= 0 ? slot : -1;
+    if (tid < n) p.slot_of[i0 + tid] = slots[tid];
+  }
+  __syncthreads();
+  for (int i = tid; i < work; i += MANY_THREADS) {
+    if (i >= MANY_THREADS) v = from[i];
+    const int token = i / p.chunks, c = i - token * p.chunks;
+    for (int j = 0; j < p.k; ++j) {
+      const int to = slots[token * p.k + j];
+      if (to >= 0) ((u32x4*)p.rows)[(int64_t)to * p.chunks + c] = v;
+    }
+  }
+}
+
 // The slots' numbers, a piece of the tokens to a workgroup.
 __global__ __launch_bounds__(THREADS) void place_rows_kernel(DispatchArgs p) {
   __shared__ Counts before, rest;
@@ -189,13 +231,13 @@ __global__ __launch_bounds__(THREADS) void place_rows_kernel(DispatchArgs p) {
   __shared__ int of_wave[WAVES][MAX_E];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t0 = (int64_t)blockIdx.x * p.piece, t1 = min(p.T, t0 + p.piece);
-  const unsigned i0 = (unsigned)(t0 * p.k), i1 = (unsigned)(t1 * p.k), all = (unsigned)(p.T * p.k);
+  const unsigned i0 = (unsigned)(t0 * p.k), i1 = (unsigned)(t1 * p.k);
   Ids<1, THREADS> ids;                       // (asked for before the counting, which takes longer than they do)
   ids.request(p, i0 + tid, i1);
   clear(&before);
   clear(&rest);
   __syncthreads();
-  if (p.counts) {
+  {
     const unsigned mine = blockIdx.x * (unsigned)p.E, n = (unsigned)p.pieces * (unsigned)p.E, e_step = THREADS % (unsigned)p.E;
     constexpr int DEEP = 8;
     unsigned e = tid % (unsigned)p.E;
@@ -210,8 +252,6 @@ __global__ __launch_bounds__(THREADS) void place_rows_kernel(DispatchArgs p) {
         if (e >= (unsigned)p.E) e -= p.E;
       }
     }
-  } else {
-    count(p, 0, i0, all, &before, &rest);
   }
   __syncthreads();
   if (tid < 64) {                            // rows of the experts in front, and of this one in front of the workgroup's
@@ -432,21 +472,21 @@ int check_4(const char* who, std::initializer_list<const void*> pointers) {
 // What the caches behind the XCDs' hold: where a call reads and writes more, the larger of its streams goes past them.
 constexpr double HELD_BYTES = 268.5e6;
 inline bool past_caches(int64_t rows, int64_t row_bytes) { return (double)rows * (double)row_bytes > HELD_BYTES; }
-// Slots up to which one launch does all of it, and up to which the workgroups that place a piece count all ids by themselves.
-constexpr int FEW_SLOTS = 1024;
-constexpr int64_t COUNT_ALL_SLOTS = 4096;
-constexpr int64_t MOST_COUNTS = 8192;        // that a workgroup adds up
-struct DispatchPlan { int piece = 0, pieces = 0; bool counted = false; };
+// Slots up to which one launch does all of it, in either of two ways.
+constexpr int FEW_SLOTS = THREADS, MANY_SLOTS = 4 * MANY_THREADS;
+constexpr int64_t MOST_COUNTS = 8192;        // of pieces and experts that a workgroup adds up
+struct DispatchPlan { int piece = 1; int64_t pieces = 0; };
 DispatchPlan plan_dispatch(int64_t T, int k, int E) {
-  DispatchPlan p;
-  if (T * k <= FEW_SLOTS) return p;
-  p.counted = T * k > COUNT_ALL_SLOTS;
+  if (T * k <= FEW_SLOTS) return {1, T > 0 ? T : 1};
+  if (T * k <= MANY_SLOTS) {                 // (as many workgroups as fit the chip; their slots are one wavefront's)
+    int piece = (int)ceil_div(T, 512);
+    return {piece, ceil_div(T, piece)};
+  }
   int64_t piece = THREADS / k;               // (a slot to a thread)
-  while (p.counted && ceil_div(T, piece) * E > MOST_COUNTS) piece *= 2;
-  p.piece = (int)piece;
-  p.pieces = (int)ceil_div(T, piece);
-  return p;
+  while (ceil_div(T, piece) * E > MOST_COUNTS) piece *= 2;
+  return {(int)piece, ceil_div(T, piece)};
 }
+static_assert(MANY_SLOTS / 512 + MAX_K <= 64, "slots of a piece");
 
 int row_shift(int chunks) {                  // lanes to a row, as a power of two
   int s = 6;
@@ -508,8 +548,7 @@ extern "C" {
 
 size_t moe_dispatch_rows_workspace(int64_t T, int k, int E) {
   if (k < 1 || k > MAX_K || E < 1 || E > MAX_E || T < 0 || T > ((int64_t)1 << 30) / k) return 0;
-  const DispatchPlan p = plan_dispatch(T, k, E);
-  return p.counted ? (size_t)p.pieces * E * sizeof(int32_t) : 0;
+  return T * k > MANY_SLOTS ? (size_t)plan_dispatch(T, k, E).pieces * E * sizeof(int32_t) : 0;
 }
 
 int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used, int64_t T, int k, int E, int H, moep_dtype dt, void* rows,
@@ -527,24 +566,23 @@ int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used
   hipStream_t s = (hipStream_t)hip_stream;
   const DispatchPlan plan = plan_dispatch(T, k, E);
   const int64_t row = (int64_t)H * (int64_t)dtype_size(dt);
-  const DispatchArgs p = {(const char*)x, experts, used, T, k, E, (int)(row / 16), plan.counted ? (int32_t*)ws : nullptr, plan.piece, plan.pieces,
-                          (char*)rows, slot_of, offsets};
-  if (!plan.pieces) {
+  const DispatchArgs p = {(const char*)x, experts, used, T, k, E, (int)(row / 16), (int32_t*)ws, plan.piece, (int)plan.pieces, (char*)rows, slot_of, offsets};
+  const dim3 grid((unsigned)plan.pieces);
+  if (T * k <= MANY_SLOTS) {
     Timed timed("dispatch_rows", s);
-    const dim3 grid((unsigned)(T > 0 ? T : 1));
-    if (T * k <= THREADS) hipLaunchKernelGGL((dispatch_few_rows_kernel<THREADS>), grid, dim3(THREADS), 0, s, p);
-    else hipLaunchKernelGGL((dispatch_few_rows_kernel<FEW_SLOTS>), grid, dim3(FEW_SLOTS), 0, s, p);
+    if (T * k <= FEW_SLOTS) hipLaunchKernelGGL(dispatch_few_rows_kernel, grid, dim3(THREADS), 0, s, p);
+    else hipLaunchKernelGGL(dispatch_many_rows_kernel, grid, dim3(MANY_THREADS), 0, s, p);
     MOEP_HIP(hipGetLastError());
     return MOEP_OK;
   }
-  if (plan.counted) {
+  {
     Timed timed("count_rows", s);
-    hipLaunchKernelGGL(count_rows_kernel, dim3((unsigned)plan.pieces), dim3(THREADS), 0, s, p);
+    hipLaunchKernelGGL(count_rows_kernel, grid, dim3(THREADS), 0, s, p);
     MOEP_HIP(hipGetLastError());
   }
   {
     Timed timed("place_rows", s);
-    hipLaunchKernelGGL(place_rows_kernel, dim3((unsigned)plan.pieces), dim3(THREADS), 0, s, p);
+    hipLaunchKernelGGL(place_rows_kernel, grid, dim3(THREADS), 0, s, p);
     MOEP_HIP(hipGetLastError());
   }
   Timed timed("copy_rows", s);
