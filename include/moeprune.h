@@ -368,7 +368,7 @@ int moe_distill_topk_backward(const void* logits, int64_t ld, const int32_t* ids
  *   slot_of [T,k] int32 (out): the row of rows that holds slot j of token t; -1 where the slot is not used
  *   offsets [E+1] int32 (out): rows offsets[e] .. offsets[e+1] - 1 are expert e's
  * A slot whose expert lies outside [0, E) is not used; a token that names an expert twice has two rows there.  T = 0: all offsets 0.
- * Workspace: moe_dispatch_rows_workspace (0 up to 4096 slots, which are one launch; beyond, three).
+ * Workspace: moe_dispatch_rows_workspace (0 up to 8192 slots, which are one launch; beyond, three).
  * moe_dispatch_rows_backward: dx [T,H] = sum over the used slots of drows [R,H], in the order of j.
  * moe_combine_rows: out [T,H] = sum over the used slots of weights[t,j] y[slot_of[t,j]], y [R,H] (the experts' output rows); a token
  *   without a used slot gives zeros.  weights [T,k] fp32, may be NULL (1).

@@ -176,8 +176,9 @@ __global__ __launch_bounds__(THREADS) void dispatch_few_rows_kernel(DispatchArgs
   }
 }
 
-// Beyond, up to MANY_THREADS x 4 slots: every workgroup counts them all, and places and copies those of `piece` tokens, 64 slots at most.
+// Beyond, up to MANY_THREADS x DEEP slots: every workgroup counts them all, and places and copies those of `piece` tokens, 64 slots at most.
 constexpr int MANY_THREADS = 1024;
+template <int DEEP>
 __global__ __launch_bounds__(MANY_THREADS) void dispatch_many_rows_kernel(DispatchArgs p) {
   __shared__ Counts before, rest;
   __shared__ int slots[64];
@@ -186,7 +187,6 @@ __global__ __launch_bounds__(MANY_THREADS) void dispatch_many_rows_kernel(Dispat
   const unsigned i0 = (unsigned)(t0 * p.k), all = (unsigned)((int)p.T * p.k);
   const int work = tokens * p.chunks;
   const u32x4* const from = (const u32x4*)p.x + (int64_t)t0 * p.chunks;
-  constexpr int DEEP = 4;
   Ids<DEEP, MANY_THREADS> ids;
   Ids<1, 64> own;
   ids.request(p, tid, all);
@@ -472,8 +472,9 @@ int check_4(const char* who, std::initializer_list<const void*> pointers) {
 // What the caches behind the XCDs' hold: where a call reads and writes more, the larger of its streams goes past them.
 constexpr double HELD_BYTES = 268.5e6;
 inline bool past_caches(int64_t rows, int64_t row_bytes) { return (double)rows * (double)row_bytes > HELD_BYTES; }
-// Slots up to which one launch does all of it, in either of two ways.
-constexpr int FEW_SLOTS = THREADS, MANY_SLOTS = 4 * MANY_THREADS;
+// Slots up to which one launch does all of it, in either of two ways.  us with the launch, in one / in three launches without the gaps between them:
+// 1024 tokens of 4096, 2 slots 9.1 / 11.0; 1999 of 2048, 4 slots (7996) 12.5 / 14.5; 4096 of 4096, 2 slots 20.7 / 22.3; 4096 of 1024, 4 slots 18.2 / 14.1.
+constexpr int FEW_SLOTS = THREADS, MANY_SLOTS = 8 * MANY_THREADS;
 constexpr int64_t MOST_COUNTS = 8192;        // of pieces and experts that a workgroup adds up
 struct DispatchPlan { int piece = 1; int64_t pieces = 0; };
 DispatchPlan plan_dispatch(int64_t T, int k, int E) {
@@ -571,7 +572,9 @@ int moe_dispatch_rows(const void* x, const int32_t* experts, const int32_t* used
   if (T * k <= MANY_SLOTS) {
     Timed timed("dispatch_rows", s);
     if (T * k <= FEW_SLOTS) hipLaunchKernelGGL(dispatch_few_rows_kernel, grid, dim3(THREADS), 0, s, p);
-    else hipLaunchKernelGGL(dispatch_many_rows_kernel, grid, dim3(MANY_THREADS), 0, s, p);
+    else if (T * k <= MANY_THREADS) hipLaunchKernelGGL(dispatch_many_rows_kernel<1>, grid, dim3(MANY_THREADS), 0, s, p);
+    else if (T * k <= 4 * MANY_THREADS) hipLaunchKernelGGL(dispatch_many_rows_kernel<4>, grid, dim3(MANY_THREADS), 0, s, p);
+    else hipLaunchKernelGGL(dispatch_many_rows_kernel<8>, grid, dim3(MANY_THREADS), 0, s, p);
     MOEP_HIP(hipGetLastError());
     return MOEP_OK;
   }

@@ -97,9 +97,9 @@ def check_sums(T, k, H, dtype, slot_of, R, seed, weighted=True):
     return got
 
 
-# one token to many pieces, one to sixteen slots, rows of one chunk to many, on both sides of 256, 1024 and 4096 slots
+# one token to many pieces, one to sixteen slots, rows of one chunk to many, on both sides of 256, 1024, 4096 and 8192 slots
 SHAPES = [(1, 1, 1, 64), (1, 2, 8, 4096), (512, 2, 8, 64), (513, 2, 8, 128), (1024, 4, 8, 64), (2, 16, 32, 128), (7, 3, 5, 192), (63, 2, 8, 320), (65, 5, 16, 64), (300, 16, 3, 64), (777, 8, 32, 1024),
-          (1025, 1, 2, 512), (2047, 4, 16, 256), (2049, 4, 16, 2048), (2050, 2, 8, 576), (4097, 2, 8, 64), (5003, 6, 32, 128), (33000, 2, 8, 64)]
+          (1025, 1, 2, 512), (2047, 4, 16, 256), (2049, 4, 16, 2048), (2050, 2, 8, 576), (2049, 2, 8, 128), (8192, 1, 8, 64), (4097, 2, 8, 64), (5003, 6, 32, 128), (33000, 2, 8, 64)]
 
 
 @pytest.mark.parametrize("use", [False, True])

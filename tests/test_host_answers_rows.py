@@ -63,11 +63,11 @@ def test_rows_refusals(call):
 
 def test_dispatch_workspaces():
     ws = binding.moe_dispatch_rows_workspace
-    assert ws(0, 2, 8) == 0 and ws(1, 16, 32) == 0 and ws(2048, 2, 8) == 0 and ws(256, 16, 32) == 0
-    assert ws(2049, 2, 8) > 0 and ws(-1, 2, 8) == 0 and ws(10, 17, 8) == 0 and ws(10, 2, 33) == 0 and ws(1 << 30, 2, 8) == 0
+    assert ws(0, 2, 8) == 0 and ws(1, 16, 32) == 0 and ws(4096, 2, 8) == 0 and ws(512, 16, 32) == 0
+    assert ws(4097, 2, 8) > 0 and ws(-1, 2, 8) == 0 and ws(10, 17, 8) == 0 and ws(10, 2, 33) == 0 and ws(1 << 30, 2, 8) == 0
     for T in (5000, 32768, 100001, 1 << 20, (1 << 26) - 1):
         for k, E in ((16, 32), (2, 8), (1, 32), (16, 1)):
-            assert 0 < ws(T, k, E) <= max(8192, 2 * E) * 4           # (one piece has to do, in the end)
+            assert (0 < ws(T, k, E) <= 8192 * 4) if T * k > 8192 else ws(T, k, E) == 0
 
 
 def policy(z=ONE, ld=100, tok=ONE, old=ONE, adv=ONE, ref=ONE, T=4, V=100, dt=1, lo=0.2, hi=0.2, kl=0.1, tau=1.0, w=None, loss=ONE, lp=ONE,
