@@ -136,7 +136,7 @@ __device__ __forceinline__ void add_group(Group& v, Running& a, float c) {
     a.m = m;
     a.near = fabsf(m * c) < 0x1p20f;
     a.k = a.near ? rintf(m * c) : 0.f;
-    a.f = a.near ? exp2_fast(a.k - m * c) : 1.f;
+    a.f = a.near ? exp2_fast(fmaf(-m, c, a.k)) : 1.f;        // (m c is not rounded, as the elements' z c are not)
   }
   float s0 = 0.f, s1 = 0.f;
   auto add = [&](auto exponent) {

@@ -207,3 +207,16 @@ int main() {
     subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=address,undefined", str(tmp_path / "search.cpp"), "-o", exe], check=True)
     r = subprocess.run([exe], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_launches_keep_to_the_grid_limits(tmp_path):
+    """Every launch at the largest sizes, noted by a program that stands in for the HIP runtime."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe, lib = str(tmp_path / "driver"), binding.library_path()
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-rdynamic", "-I", os.path.join(root, "include"),
+                        os.path.join(root, "tests", "host_answers_rows_driver.cpp"), "-o", exe, lib, "-Wl,-rpath," + os.path.dirname(lib),
+                        "-Wl,-rpath-link,/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-Wl,--unresolved-symbols=ignore-in-shared-libs"],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "all checks passed", (r.stdout[-4000:], r.stderr[-2000:])
