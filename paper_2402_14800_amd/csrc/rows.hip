@@ -293,7 +293,7 @@ __global__ __launch_bounds__(THREADS) void copy_rows_kernel(DispatchArgs p, int 
   const int64_t t = group * side + (lane >> shift);
   const int c = (int)(item - group * parts) * (1 << shift) + (lane & ((1 << shift) - 1));
   if (t >= p.T || c >= p.chunks) return;
-  const u32x4 v = ((const u32x4*)p.x)[t * p.chunks + c];
+  const u32x4 v = load<STREAM>((const u32x4*)p.x + t * p.chunks + c);
   for (int j0 = 0; j0 < p.k; j0 += KG) {
     int slot[KG];
 #pragma unroll
