@@ -9,6 +9,8 @@
 //                loss = -(1 - ls) log sigmoid(h) - ls log sigmoid(-h), c = +-(ls - sigmoid(-h)) beta (over the number of tokens)
 // Bound by the read of the logits and the write of the gradient.  The policy loss knows c as soon as its row is summed, so the row stays in
 // registers and is read once; a pair's c needs all rows of both answers, so the gradient reads the logits again, last rows first.
+// us and bytes read and written: policy loss and gradient of 4096 rows of 32000 bf16 93 (5.6 TB/s); loss, then gradient of 1001 of 50001 22 (4.7) and 31
+// (6.5); pairs of 3333 rows of 32000 32 to 36 (6.2 where the call before left something in the caches), 4.9 for the 8 pairs, 63 to 67 (6.5).
 #include "logits_rows.h"
 
 namespace moep {
