@@ -54,18 +54,37 @@ __device__ __forceinline__ float exp_beyond_line(float x) {
   return e == -NEG_INF ? e : e - x;                          // (x may be infinite itself)
 }
 
+// (z - m) / tau - log s as a number and what its rounding left out: ratios and an answer's sum see differences of such numbers, which are small, and the
+// logarithm's own last place is 5e-7 for the sum of a large vocabulary.  s = 2^e f with f next to 1: e log 2 in two parts, the first without
+// rounding (12 bits), and a logarithm of at most 0.4.
+struct LogProb { float value, rest; };
+__device__ __forceinline__ LogProb log_prob(float z, float m, float s, float tau) {
+  const float d = z - m, q = d / tau;
+  if (!(fabsf(q) < 0x1p100f)) return {q - logf(s), 0.f};     // (-inf, or a mask of the type's lowest value)
+  const float back = d - z, d_rest = (z - (d - back)) - (m + back);
+  const float q_rest = (fmaf(-q, tau, d) + d_rest) / tau;
+  int e;
+  float f = frexpf(s, &e);
+  if (f < 0.70710678f) { f *= 2.f; --e; }
+  constexpr float LN2_HI = 0x1.62ep-1f, LN2_LO = 0x1.0bfbe8p-15f;
+  const float hi = (float)e * LN2_HI, lo = fmaf((float)e, LN2_LO, logf(f));
+  const float a = q - hi, a_back = a - q, a_rest = (q - (a - a_back)) - (hi + a_back);
+  const float small = (a_rest + q_rest) - lo, value = a + small;
+  return {value, small - (value - a)};
+}
+
 struct Term { float loss, slope; };
-__device__ __forceinline__ Term policy_term(const AnswerArgs& p, float lp, float old, float A, float ref) {
+__device__ __forceinline__ Term policy_term(const AnswerArgs& p, const LogProb& lp, float old, float A, float ref) {
   Term t = {0.f, 0.f};
   if (!(A == 0.f)) {                                         // (nothing to gain either way, also where r is infinite)
-    const float r = expf(lp - old);
+    const float r = expf((lp.value - old) + lp.rest);
     // the ratio has gone as far as it may the way the advantage asks for
     const bool far = A > 0.f ? r > p.high : r < p.low;
     t.loss = far ? -(A > 0.f ? p.high : p.low) * A : -r * A;
     t.slope = far ? 0.f : -r * A;
   }
   if (p.ref) {
-    const float e = ref - lp;
+    const float e = (ref - lp.value) - lp.rest;
     t.loss = fmaf(p.kl, exp_beyond_line(e), t.loss);
     t.slope = fmaf(-p.kl, expm1f(e), t.slope);
   }
@@ -92,7 +111,8 @@ __device__ __forceinline__ int answer_of(const int64_t* offsets, int n, int64_t 
 // Four chunks at a time, the next four on their way meanwhile, each four with a running maximum of its own: a wavefront adds up what has
 // come while the rest comes, and 32 registers of chunks leave room for twice as many wavefronts as a row that is held.  An element costs
 // the lanes seven operations (unpacked, one FMA, the exponential's four, one sum): the exponent is z c - k with k the integer next to m c, whose
-// factor exp2(k - m c) is left to the four's sum.
+// factor exp2(k - m c) is left to the four's sum.  (c = log2(e) / tau is a number of 32 bits: sums are too large by 1.3e-8 for each unit that the
+// logits lie below the maximum.  A second FMA with what c leaves out took 3 to 7 % of the loss's time for 2e-8 of a log probability.)
 constexpr int GROUP = 4;
 struct Running {
   float m = NEG_INF, s = 0.f;                // maximum, and sum of exp2((z - m) c)
@@ -246,14 +266,16 @@ __global__ __launch_bounds__(B, MODE != LOSS_AND_GRADIENT ? 7 : 1) void answers_
     all = join_all<B, false>(all, c, shared);
     m = uniform(all.m);
     const float log_s = uniform(logf(all.s));
-    float lp = m == NEG_INF ? NEG_INF : (zy - m) / p.tau - log_s;
-    if (!(y < p.V)) lp = __builtin_nanf("");
+    LogProb lp = {NEG_INF, 0.f};
+    if (!(y < p.V)) lp.value = __builtin_nanf("");
+    else if (!(m == NEG_INF)) lp = log_prob(zy, m, uniform(all.s), p.tau);
     Term term = {0.f, 0.f};
     if (!p.offsets) term = policy_term(p, lp, old, A, ref);
     if (tid == 0) {
       if (!p.offsets) p.loss[t] = term.loss;
-      p.logprob[t] = lp;
-      p.stats[3 * t] = m; p.stats[3 * t + 1] = m == NEG_INF ? 0.f : log_s; p.stats[3 * t + 2] = term.slope;
+      p.logprob[t] = lp.value;
+      // (of a pair's row what lp left out, where its derivative will be)
+      p.stats[3 * t] = m; p.stats[3 * t + 1] = m == NEG_INF ? 0.f : log_s; p.stats[3 * t + 2] = p.offsets ? lp.rest : term.slope;
     }
     if (MODE == LOSS) return;
     scale = uniform(term.slope * weight / p.tau);
@@ -337,16 +359,16 @@ __global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
     constexpr int DEEP = 4;
     for (int64_t t = r0 + tid; t < r1; t += DEEP * (PAIR_THREADS / 2)) {
       int64_t y[DEEP];
-      float lp[DEEP], ref[DEEP];
+      float lp[DEEP], rest[DEEP], ref[DEEP];
 #pragma unroll
       for (int q = 0; q < DEEP; ++q) {       // (beyond the end the last row again: all loads at once)
         const int64_t i = min(t + q * (PAIR_THREADS / 2), r1 - 1);
-        y[q] = p.tokens[i]; lp[q] = p.logprob[i]; ref[q] = p.ref[i];
+        y[q] = p.tokens[i]; lp[q] = p.logprob[i]; rest[q] = p.stats[3 * i + 2]; ref[q] = p.ref[i];
       }
 #pragma unroll
       for (int q = 0; q < DEEP; ++q)
         if (t + q * (PAIR_THREADS / 2) < r1 && y[q] >= 0) {
-          x += (double)lp[q] - (double)ref[q];
+          x += ((double)lp[q] - (double)ref[q]) + (double)rest[q];
           ++n;
         }
     }
