@@ -432,7 +432,8 @@ int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* toke
  *   grad [T,V] dt (out, may be NULL): weights[i] times the gradient of loss[i] by the logits of its answers' rows; memory as in
  *     moe_distill_topk.  0 for their rows without a token; rows outside all answers are left as they were
  *   weights [pairs] fp32, may be NULL (1)
- * Sums over an answer are fp64, of log probabilities that are off by about 1e-7 each.  The logits are read twice where the gradient is wanted: a pair's derivative needs both whole answers.
+ * Sums over an answer are fp64, of log probabilities that are off by about 1e-7 each.  The logits are read twice where the
+ * gradient is wanted: a pair's derivative needs both whole answers.
  * A token of probability 0 makes its pair's loss what the formula gives: infinite, 0, or (both answers) NaN, and the derivative with it.
  * moe_preference_loss_backward: the gradient alone, from the stats and grad_loss [pairs] fp32 (rows where it is 0 are not read and get
  * 0).  grad may be the logits' own memory in both. */

@@ -83,6 +83,7 @@ __device__ __forceinline__ int total(const Counts& c, int e) {
   for (int q = 0; q < COPIES; ++q) n += c.n[q][e];
   return n;
 }
+
 __global__ __launch_bounds__(THREADS) void count_rows_kernel(DispatchArgs p) {
   __shared__ Counts c;
   clear(&c);
