@@ -76,7 +76,7 @@ __device__ __forceinline__ LogProb log_prob(float z, float m, float s, float tau
 struct Term { float loss, slope; };
 __device__ __forceinline__ Term policy_term(const AnswerArgs& p, const LogProb& lp, float old, float A, float ref) {
   Term t = {0.f, 0.f};
-  if (!(A == 0.f)) {                                         // (nothing to gain either way, also where r is infinite)
+  if (!(A == 0.f) || lp.value != lp.value) {                 // (A = 0: nothing to gain either way, also where r is infinite)
     const float r = expf((lp.value - old) + lp.rest);
     // the ratio has gone as far as it may the way the advantage asks for
     const bool far = A > 0.f ? r > p.high : r < p.low;

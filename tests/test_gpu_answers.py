@@ -192,6 +192,20 @@ def test_policy_beyond_its_range(V, dtype):
         check_policy(z[7:], tokens[7:], old[7:], A[7:], ref[7:], kl=kl)
 
 
+@pytest.mark.parametrize("kl", [0.0, 0.1])
+def test_an_advantage_of_zero_hides_no_nan(kl):
+    """A token that does not exist, and NaN in a row, show in its loss and gradient whatever the advantage."""
+    z = make_logits(3, 70, F32, seed=18)
+    z[1, 69] = float("nan")
+    tokens = torch.tensor([70, 3, 3], device=DEV)
+    old, A, ref, _ = make_policy(z[2:].expand(3, 70), torch.full((3,), 3), 1.0, seed=19)
+    loss, lp, stats, grad = pkg.moe_policy_loss(z, tokens, old, torch.zeros_like(A), ref, kl=kl, gradient=True)
+    back = pkg.moe_policy_loss_backward(z, tokens, stats, torch.ones(3, device=DEV))
+    for got in (loss, lp, grad, back):
+        assert bool(torch.isnan(got[:2]).all()) and bool(torch.isfinite(got[2]).all())
+    assert kl or (float(loss[2]) == 0.0 and not bool(grad[2].any()))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("tau", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
 def test_policy_at_the_temperatures_ends(tau, dtype):
