@@ -403,8 +403,8 @@ int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* sl
  *     moe_distill_topk (may be the logits' own, with ld_grad = ld)
  *   weights [T] fp32, may be NULL (1)
  * A row with a negative token (a prompt's, or padding) or of weight 0 is left out: its logits, and with a negative token what else
- * belongs to it, count for nothing; loss, logprob and gradient are 0, stats -inf, 0, 0.  A token of V or more: NaN.  An advantage of 0 leaves
- * the KL term alone, however large r.  Where the clip holds, the first term's derivative is 0 (at r = the bound itself it does not hold).
+ * belongs to it, count for nothing; loss, logprob and gradient are 0, stats -inf, 0, 0.  A token of V or more, or an advantage of NaN: NaN.  An
+ * advantage of 0 leaves the KL term alone, however large r.  Where the clip holds, the first term's derivative is 0 (at r = the bound itself it does not hold).
  * A loss beyond 32 bits is infinite (a KL term with a token of probability 0, say, or a negative advantage with an r that is), and its
  * row's gradient 0.
  * moe_policy_loss_backward: the gradient alone, from the stats and the upstream gradient of every loss, grad_loss [T] fp32 (a row where

@@ -79,7 +79,7 @@ __device__ __forceinline__ Term policy_term(const AnswerArgs& p, const LogProb& 
   if (!(A == 0.f) || lp.value != lp.value) {                 // (A = 0: nothing to gain either way, also where r is infinite)
     const float r = expf((lp.value - old) + lp.rest);
     // the ratio has gone as far as it may the way the advantage asks for
-    const bool far = A > 0.f ? r > p.high : r < p.low;
+    const bool far = A > 0.f ? r > p.high : A < 0.f && r < p.low;   // (NaN asks for neither)
     t.loss = far ? -(A > 0.f ? p.high : p.low) * A : -r * A;
     t.slope = far ? 0.f : -r * A;
   }
