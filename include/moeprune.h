@@ -430,13 +430,15 @@ int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* toke
  *   logprob [T] fp32 (out), stats [T,3] fp32 (out): as in moe_policy_loss, the derivative being that of the row's pair; 0 and -inf, 0, 0
  *     for rows without a token or outside all answers, whose logits are not read
  *   grad [T,V] dt (out, may be NULL): weights[i] times the gradient of loss[i] by the logits of its answers' rows; memory as in
- *     moe_distill_topk.  0 for their rows without a token; rows outside all answers are left as they were
+ *     moe_distill_topk.  0 for their rows without a token; rows outside all answers (all rows, without pairs) are left as they were
  *   weights [pairs] fp32, may be NULL (1)
  * Sums over an answer are fp64, of log probabilities that are off by about 1e-7 each.  The logits are read twice where the
  * gradient is wanted: a pair's derivative needs both whole answers.
  * A token of probability 0 makes its pair's loss what the formula gives: infinite, 0, or (both answers) NaN, and the derivative with it.
  * moe_preference_loss_backward: the gradient alone, from the stats and grad_loss [pairs] fp32 (rows where it is 0 are not read and get
- * 0).  grad may be the logits' own memory in both. */
+ * 0).  grad may be the logits' own memory in both.
+ * moe_preference_loss_all_rows, moe_preference_loss_backward_all_rows: the same two calls for a gradient in memory that holds nothing yet.
+ * Its rows outside all answers are written too, with 0; grad may not be NULL. */
 int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
                         const float* ref_logprob, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, float beta,
                         float smoothing, int average, const float* weights, float* loss, float* rewards,
@@ -444,6 +446,14 @@ int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, c
 int moe_preference_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
                                  const float* stats, const float* grad_loss, int64_t T, int64_t V, int64_t pairs,
                                  moep_dtype dt, void* grad, int64_t ld_grad, void* hip_stream);
+int moe_preference_loss_all_rows(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
+                                 const float* ref_logprob, int64_t T, int64_t V, int64_t pairs, moep_dtype dt,
+                                 float beta, float smoothing, int average, const float* weights, float* loss,
+                                 float* rewards, float* logprob, float* stats, void* grad, int64_t ld_grad,
+                                 void* hip_stream);
+int moe_preference_loss_backward_all_rows(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets,
+                                          const float* stats, const float* grad_loss, int64_t T, int64_t V,
+                                          int64_t pairs, moep_dtype dt, void* grad, int64_t ld_grad, void* hip_stream);
 
 /* ---- per-kernel timing (for benchmarks) ------------------------------------ */
 /* While enabled, every kernel launch is bracketed by HIP events on its stream.

@@ -37,6 +37,7 @@ EXPORTS = (
     "expert_ffn_forward_workspace", "expert_ffn_forward", "expert_ffn_backward_workspace", "expert_ffn_backward",
     "moe_dispatch_rows_workspace", "moe_dispatch_rows", "moe_dispatch_rows_backward", "moe_combine_rows", "moe_combine_rows_backward",
     "moe_policy_loss", "moe_policy_loss_backward", "moe_preference_loss", "moe_preference_loss_backward",
+    "moe_preference_loss_all_rows", "moe_preference_loss_backward_all_rows",
     "moep_timing_enable", "moep_timing_collect", "moep_timing_records", "moep_mfma_ceiling",
 )
 
@@ -172,6 +173,9 @@ def _load() -> ctypes.CDLL:
     lib.moe_preference_loss_backward.restype = c_int
     lib.moe_preference_loss_backward.argtypes = [c_void_p, c_int64] + [c_void_p] * 4 + [c_int64, c_int64, c_int64, c_int, c_void_p, c_int64,
                                                                                          c_void_p]
+    for whole, like in ((lib.moe_preference_loss_all_rows, lib.moe_preference_loss),
+                        (lib.moe_preference_loss_backward_all_rows, lib.moe_preference_loss_backward)):
+        whole.restype, whole.argtypes = like.restype, like.argtypes
     lib.moep_timing_enable.restype = c_int
     lib.moep_timing_enable.argtypes = [c_int]
     lib.moep_timing_collect.restype = c_int
@@ -835,7 +839,7 @@ def moe_preference_loss(logits, tokens, offsets, ref_logprob, beta: float = 0.1,
     """loss [P], rewards [2,P], logprob [T] and stats [T,3] (fp32) of P pairs of answers: answer a is rows offsets[a] .. offsets[a+1] - 1 of
     logits [T,V], offsets [2 P + 1] int64; pair i is answers i (chosen) and P + i (rejected); tokens [T] int64 (negative: none), ref_logprob
     [T] fp32.  With `gradient` also the gradient of (weights * loss).sum(), weights [P], by the logits, into `out` if given (which may be
-    `logits`); its rows outside all answers stay as they were (without `out`: are not initialised)."""
+    `logits`): its rows outside all answers stay as they were in `out`, and are 0 without it."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
     dev = logits.device
@@ -847,7 +851,8 @@ def moe_preference_loss(logits, tokens, offsets, ref_logprob, beta: float = 0.1,
     loss, rewards = _empty(P, dtype=torch.float32, device=dev), _empty(2, P, dtype=torch.float32, device=dev)
     logprob, stats = _empty(T, dtype=torch.float32, device=dev), _empty(T, 3, dtype=torch.float32, device=dev)
     grad, ld_grad = _gradient_rows(logits, out, T, V) if gradient else (None, 0)
-    _call_on(dev, _lib.moe_preference_loss, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), ref_logprob.data_ptr(), T, V, P, dt, beta,
+    call = _lib.moe_preference_loss_all_rows if gradient and out is None else _lib.moe_preference_loss
+    _call_on(dev, call, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), ref_logprob.data_ptr(), T, V, P, dt, beta,
              smoothing, 1 if average else 0, _ptr(weights), loss.data_ptr(), rewards.data_ptr(), logprob.data_ptr(), stats.data_ptr(), _ptr(grad),
              ld_grad)
     return (loss, rewards, logprob, stats, grad) if gradient else (loss, rewards, logprob, stats)
@@ -855,7 +860,7 @@ def moe_preference_loss(logits, tokens, offsets, ref_logprob, beta: float = 0.1,
 
 def moe_preference_loss_backward(logits, tokens, offsets, stats, grad_loss, out=None):
     """The gradient [T,V] by the logits, from moe_preference_loss's stats and the upstream gradient [P] fp32 of its loss.  Rows outside all
-    answers stay as they were in `out` (without it: are not initialised)."""
+    answers stay as they were in `out`, and are 0 without it."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
     dev = logits.device
@@ -864,7 +869,8 @@ def moe_preference_loss_backward(logits, tokens, offsets, stats, grad_loss, out=
     _beside(stats, (T, 3), torch.float32, dev.index, "stats")
     _beside(grad_loss, (P,), torch.float32, dev.index, "grad_loss")
     grad, ld_grad = _gradient_rows(logits, out, T, V)
-    _call_on(dev, _lib.moe_preference_loss_backward, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), stats.data_ptr(),
+    call = _lib.moe_preference_loss_backward_all_rows if out is None else _lib.moe_preference_loss_backward
+    _call_on(dev, call, logits.data_ptr(), ld, tokens.data_ptr(), offsets.data_ptr(), stats.data_ptr(),
              grad_loss.data_ptr(), T, V, P, dt, grad.data_ptr(), ld_grad)
     return grad
 

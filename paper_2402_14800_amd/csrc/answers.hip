@@ -35,6 +35,7 @@ struct AnswerArgs {
   int64_t stream_rows;                       // the launch's first rows are read past the caches: so many of them
   bool stream_grad;                          // and the gradient is written past them
   int parts, span;                           // GRADIENT: workgroups to a row, and chunks to each of them
+  bool all_rows;                             // GRADIENT, preference: rows of no answer get 0, and are not left as they were
 };
 
 // exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, 1e-9 of the sum.)
@@ -291,7 +292,10 @@ __global__ __launch_bounds__(B, MODE != LOSS_AND_GRADIENT ? 7 : 1) void answers_
     float up = 1.f;
     if (p.offsets) {
       const int pairs = (int)p.pairs, a = answer_of(p.offsets, 2 * pairs + 1, p.first + t);
-      if (a < 0 || a >= 2 * pairs) return;                   // a row of no answer: as it was
+      if (a < 0 || a >= 2 * pairs) {                         // a row of no answer
+        if (p.all_rows) write_zeros();
+        return;
+      }
       if (p.up) up = uniform(p.up[a < pairs ? a : a - pairs]);
     } else if (p.up) {
       up = uniform(p.up[t]);
@@ -488,6 +492,53 @@ int check_scalars(const char* who, std::initializer_list<const void*> of4, std::
   return MOEP_OK;
 }
 
+// `all_rows`: the gradient's rows of no answer are written too, with 0.
+int preference_loss(const char* who, const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* ref_logprob, int64_t T,
+                    int64_t V, int64_t pairs, moep_dtype dt, float beta, float smoothing, int average, const float* weights, float* loss,
+                    float* rewards, float* logprob, float* stats, void* grad, int64_t ld_grad, bool all_rows, hipStream_t s) {
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
+  if (!(beta > 0.f && beta <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: beta %g out of range (0, 2^60]", who, (double)beta);
+  if (!(smoothing >= 0.f && smoothing < 1.f)) return fail(MOEP_EINVAL, "%s: smoothing %g out of range [0, 1)", who, (double)smoothing);
+  if (average != 0 && average != 1) return fail(MOEP_EINVAL, "%s: average=%d is neither 0 nor 1", who, average);
+  if (grad)
+    if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (!offsets) return fail(MOEP_EINVAL, "%s: NULL offsets", who);
+  if (pairs > 0 && (!loss || !rewards)) return fail(MOEP_EINVAL, "%s: NULL loss or rewards", who);
+  if (T > 0 && (!logits || !tokens || !ref_logprob || !logprob || !stats))
+    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, ref_logprob, logprob or stats", who);
+  if (int st = check_scalars(who, {ref_logprob, weights, loss, rewards, logprob, stats}, {tokens, offsets})) return st;
+  AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, nullptr, offsets, pairs, 0,
+                  nullptr, logprob, stats, nullptr, 0};
+  if (T > 0)
+    if (int st = launch_answers<LOSS>(p, T, dt, s, "answer_logprobs")) return st;
+  if (pairs > 0) {
+    Timed timed("pairs", s);
+    const PairArgs q = {tokens, offsets, ref_logprob, logprob, T, pairs, beta, smoothing, average, loss, rewards, stats};
+    hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)pairs), dim3(PAIR_THREADS), 0, s, q);
+    MOEP_HIP(hipGetLastError());
+  }
+  if (!grad || T == 0 || (pairs == 0 && !all_rows)) return MOEP_OK;
+  p.up = weights; p.grad = grad; p.ld_grad = ld_grad; p.all_rows = all_rows;
+  return launch_answers<GRADIENT>(p, T, dt, s, "preference_gradient");
+}
+
+int preference_gradient(const char* who, const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* stats,
+                        const float* grad_loss, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, void* grad, int64_t ld_grad, bool all_rows,
+                        hipStream_t s) {
+  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
+  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
+  if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
+  if (T == 0 || (pairs == 0 && !all_rows)) return MOEP_OK;
+  if (!logits || !tokens || !offsets || !stats || (pairs > 0 && !grad_loss) || !grad)
+    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, offsets, stats, grad_loss or grad", who);
+  if (int st = check_scalars(who, {stats, grad_loss}, {tokens, offsets})) return st;
+  AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, grad_loss, offsets, pairs, 0,
+                  nullptr, nullptr, (float*)stats, grad, ld_grad};
+  p.all_rows = all_rows;
+  return launch_answers<GRADIENT>(p, T, dt, s, "preference_gradient");
+}
+
 }  // namespace
 }  // namespace moep
 
@@ -534,49 +585,32 @@ int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* toke
 int moe_preference_loss(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* ref_logprob, int64_t T,
                         int64_t V, int64_t pairs, moep_dtype dt, float beta, float smoothing, int average, const float* weights, float* loss,
                         float* rewards, float* logprob, float* stats, void* grad, int64_t ld_grad, void* hip_stream) {
-  const char* who = "moe_preference_loss";
-  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
-  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
-  if (!(beta > 0.f && beta <= 0x1p60f)) return fail(MOEP_EINVAL, "%s: beta %g out of range (0, 2^60]", who, (double)beta);
-  if (!(smoothing >= 0.f && smoothing < 1.f)) return fail(MOEP_EINVAL, "%s: smoothing %g out of range [0, 1)", who, (double)smoothing);
-  if (average != 0 && average != 1) return fail(MOEP_EINVAL, "%s: average=%d is neither 0 nor 1", who, average);
-  if (grad)
-    if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
-  if (!offsets) return fail(MOEP_EINVAL, "%s: NULL offsets", who);
-  if (pairs > 0 && (!loss || !rewards)) return fail(MOEP_EINVAL, "%s: NULL loss or rewards", who);
-  if (T > 0 && (!logits || !tokens || !ref_logprob || !logprob || !stats))
-    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, ref_logprob, logprob or stats", who);
-  if (int st = check_scalars(who, {ref_logprob, weights, loss, rewards, logprob, stats}, {tokens, offsets})) return st;
-  hipStream_t s = (hipStream_t)hip_stream;
-  AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, nullptr, offsets, pairs, 0,
-                  nullptr, logprob, stats, nullptr, 0};
-  if (T > 0)
-    if (int st = launch_answers<LOSS>(p, T, dt, s, "answer_logprobs")) return st;
-  if (pairs > 0) {
-    Timed timed("pairs", s);
-    const PairArgs q = {tokens, offsets, ref_logprob, logprob, T, pairs, beta, smoothing, average, loss, rewards, stats};
-    hipLaunchKernelGGL(pairs_kernel, dim3((unsigned)pairs), dim3(PAIR_THREADS), 0, s, q);
-    MOEP_HIP(hipGetLastError());
-  }
-  if (!grad || T == 0 || pairs == 0) return MOEP_OK;
-  p.up = weights; p.grad = grad; p.ld_grad = ld_grad;
-  return launch_answers<GRADIENT>(p, T, dt, s, "preference_gradient");
+  return preference_loss("moe_preference_loss", logits, ld, tokens, offsets, ref_logprob, T, V, pairs, dt, beta, smoothing, average, weights, loss,
+                         rewards, logprob, stats, grad, ld_grad, false, (hipStream_t)hip_stream);
+}
+
+int moe_preference_loss_all_rows(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* ref_logprob,
+                                 int64_t T, int64_t V, int64_t pairs, moep_dtype dt, float beta, float smoothing, int average,
+                                 const float* weights, float* loss, float* rewards, float* logprob, float* stats, void* grad, int64_t ld_grad,
+                                 void* hip_stream) {
+  const char* who = "moe_preference_loss_all_rows";
+  if (T > 0 && !grad) return fail(MOEP_EINVAL, "%s: NULL grad", who);
+  return preference_loss(who, logits, ld, tokens, offsets, ref_logprob, T, V, pairs, dt, beta, smoothing, average, weights, loss, rewards, logprob,
+                         stats, grad, ld_grad, true, (hipStream_t)hip_stream);
 }
 
 int moe_preference_loss_backward(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* stats,
                                  const float* grad_loss, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, void* grad, int64_t ld_grad,
                                  void* hip_stream) {
-  const char* who = "moe_preference_loss_backward";
-  if (int st = check_rows(who, T, V, dt, logits, ld)) return st;
-  if (pairs < 0 || pairs > (int64_t)1 << 22) return fail(MOEP_EINVAL, "%s: %lld pairs out of range [0, 2^22]", who, (long long)pairs);
-  if (int st = check_rows(who, T, V, dt, grad, ld_grad)) return st;
-  if (T == 0 || pairs == 0) return MOEP_OK;
-  if (!logits || !tokens || !offsets || !stats || !grad_loss || !grad)
-    return fail(MOEP_EINVAL, "%s: NULL logits, tokens, offsets, stats, grad_loss or grad", who);
-  if (int st = check_scalars(who, {stats, grad_loss}, {tokens, offsets})) return st;
-  const AnswerArgs p = {logits, ld, T, (int)V, tokens, 1.f, nullptr, nullptr, nullptr, 0.f, 0.f, 0.f, grad_loss, offsets, pairs, 0,
-                        nullptr, nullptr, (float*)stats, grad, ld_grad};
-  return launch_answers<GRADIENT>(p, T, dt, (hipStream_t)hip_stream, "preference_gradient");
+  return preference_gradient("moe_preference_loss_backward", logits, ld, tokens, offsets, stats, grad_loss, T, V, pairs, dt, grad, ld_grad, false,
+                             (hipStream_t)hip_stream);
+}
+
+int moe_preference_loss_backward_all_rows(const void* logits, int64_t ld, const int64_t* tokens, const int64_t* offsets, const float* stats,
+                                          const float* grad_loss, int64_t T, int64_t V, int64_t pairs, moep_dtype dt, void* grad, int64_t ld_grad,
+                                          void* hip_stream) {
+  return preference_gradient("moe_preference_loss_backward_all_rows", logits, ld, tokens, offsets, stats, grad_loss, T, V, pairs, dt, grad, ld_grad,
+                             true, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"
