@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2402_14800_amd as pkg
-from tests.test_gpu_answers import BF16, DEV, F32, make_pairs, make_policy, reference
+from tests.test_gpu_answers import BF16, DEV, F32, INF, make_pairs, make_policy, reference
 from tests.test_gpu_logits import make_logits
 
 pytestmark = pytest.mark.gpu
@@ -91,3 +91,80 @@ def test_rows_of_no_answer_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+# ---------------------------------------------------------------- what 32 bits of a log probability leave out
+# Rows of n zeros, all else masked with -inf, and the token's logit at -60 tau: every term of the row's sum is 1 or (exp(-60) = 9e-27) nothing, so the sum is n without
+# an error (n < 2^24), and lp = -60 - log n has a last place of 2^-17, 7.6e-6.  The two parts of lp together: a logarithm of at most 0.35 (2 units of 2^-25),
+# the fma and the sum behind it (2^-26 each): under 2^-23.  Of a temperature, d / tau is off by half a unit of 64 (2^-19), which the second part takes up to 2^-24 of it.
+N_ROWS = 4096
+LP = 2.0 ** -23
+
+
+def flat_rows(dtype, V, tau=1.0, seed=80):
+    """The rows, their tokens and, in 64 bits, lp."""
+    g = torch.Generator().manual_seed(seed)
+    n = torch.randint(1, V - 1, (N_ROWS,), generator=g)
+    z = torch.zeros((N_ROWS, V))
+    z[torch.arange(V)[None] >= n[:, None]] = -INF
+    low = float(torch.tensor(-60.0 * tau).to(dtype))
+    z[:, V - 1] = low
+    tau = float(torch.tensor(tau, dtype=F32))
+    return z.to(dtype).to(DEV), torch.full((N_ROWS,), V - 1, device=DEV), low / tau - n.double().log(), n
+
+
+@pytest.mark.parametrize("held", [True, False])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,tau", [(1003, 1.0), (5003, 0.7), (32003, 1.3)])
+def test_ratios_keep_what_32_bits_of_a_log_probability_leave_out(V, tau, dtype, held):
+    """old is lp to the nearest in 32 bits, so that log r is what that left out, up to 3.8e-6 and 2e-6 in the mean.  r A is then off by LP, an
+    exponential next to 1 (2 units of 2^-23) and a product (2^-24): under 2^-21 = 4.8e-7 of A.  With lp of 32 bits alone most rows would be beyond it."""
+    z, tokens, lp, _ = flat_rows(dtype, V, tau)
+    old = lp.float()
+    A = (torch.rand(N_ROWS, generator=torch.Generator().manual_seed(81)) + 0.5) * torch.tensor([1.0, -1.0])[torch.arange(N_ROWS) % 2]
+    r = torch.exp(lp - old.double())
+    assert float(((r - 1).abs() > 2.0 ** -21).double().mean()) > 0.5          # (what r = 1 would be off by)
+    args = (z, tokens, old.to(DEV), A.to(DEV))
+    if held:                                                 # the row in registers, the gradient with it
+        loss, got, stats, grad = pkg.moe_policy_loss(*args, temperature=tau, gradient=True)
+    else:
+        loss, got, stats = pkg.moe_policy_loss(*args, temperature=tau)
+    want = -r * A.double()
+    assert bool(((got.double().cpu() - lp).abs() <= 2.0 ** -18 + LP).all())
+    for x in (loss, stats[:, 2]):
+        assert bool(((x.double().cpu() - want).abs() <= 2.0 ** -21 * A.double().abs()).all()), float(((x.double().cpu() - want) / A).abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_small_kl_distance_keeps_what_32_bits_of_a_log_probability_leave_out(dtype):
+    """Advantage 0 and a reference next to the model: exp(e) - e - 1 = e^2 / 2 and up with e off by LP, so by 2 LP / |e| of itself (and LP^2 / 2 where e is as small)
+    and 2^-20 for the series and its products."""
+    z, tokens, lp, _ = flat_rows(dtype, 4001)
+    zero = torch.zeros(N_ROWS, device=DEV)
+    ref = (lp + 1e-3 * torch.randn(N_ROWS, generator=torch.Generator().manual_seed(82))).float()
+    e = ref.double() - lp
+    want = torch.expm1(e) - e
+    loss = pkg.moe_policy_loss(z, tokens, zero, zero, ref.to(DEV), kl=1.0)[0].double().cpu()
+    bound = (2 * LP * e.abs() + LP * LP) * torch.exp(e.abs()) + 2.0 ** -20 * want
+    rough = ref.double() - lp.float().double()
+    assert float(((torch.expm1(rough) - rough - want).abs() > bound).double().mean()) > 0.5   # (with lp of 32 bits alone)
+    assert bool(((loss - want).abs() <= bound).all()), float(((loss - want).abs() - bound).max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("average", [False, True])
+def test_a_long_answers_reward_keeps_what_32_bits_of_its_log_probabilities_leave_out(average, dtype):
+    """Rows that are all alike, so that what 32 bits leave out of one is left out of all: the reward of n rows is off by n LP (LP with `average`), and
+    2^-24 of itself."""
+    z, tokens, lp, n = flat_rows(dtype, 2003)
+    worst = int((lp - lp.float().double()).abs().argmax())
+    z, lp = z[worst:worst + 1].expand(N_ROWS, -1).contiguous(), float(lp[worst])
+    ref = torch.full((N_ROWS,), lp, dtype=F32)
+    rows = [N_ROWS - 100, 100]
+    offsets = torch.tensor([0, rows[0], N_ROWS], device=DEV)
+    left_out = lp - float(ref[0])
+    want = torch.tensor([left_out * (1 if average else m) for m in rows], dtype=torch.float64)
+    bound = torch.tensor([LP * (1 if average else m) for m in rows], dtype=torch.float64) + 2.0 ** -24 * want.abs()
+    assert bool((want.abs() > 8 * bound).all())              # (with lp of 32 bits alone the rewards are 0)
+    loss, rewards, *_ = pkg.moe_preference_loss(z, tokens, offsets, ref.to(DEV), beta=1.0, average=average)
+    assert bool(((rewards.double().cpu()[:, 0] - want).abs() <= bound).all()), (rewards[:, 0].tolist(), want.tolist())
