@@ -401,10 +401,12 @@ int moe_combine_rows_backward(const void* dout, const void* y, const int32_t* sl
  *     backward call
  *   grad [T,V] dt (out, may be NULL): weights[t] times the gradient of loss[t] by the row's logits; rows and memory as in
  *     moe_distill_topk (may be the logits' own, with ld_grad = ld)
- *   weights [T] fp32, may be NULL (1)
+ *   weights [T] fp32, may be NULL (1): of the gradient; loss and logprob do not depend on them, but for a weight of 0
  * A row with a negative token (a prompt's, or padding) or of weight 0 is left out: its logits, and with a negative token what else
- * belongs to it, count for nothing; loss, logprob and gradient are 0, stats -inf, 0, 0.  A token of V or more, or an advantage of NaN: NaN.  An
- * advantage of 0 leaves the KL term alone, however large r.  Where the clip holds, the first term's derivative is 0 (at r = the bound itself it does not hold).
+ * belongs to it, count for nothing; loss, logprob and gradient are 0, stats -inf, 0, 0.  (A pair of weight 0 in moe_preference_loss keeps its
+ * loss, and a row whose grad_loss is 0 in the backward call had one: there it is the gradient alone that is 0.)  A token of V or more, or an
+ * advantage of NaN: NaN.  An advantage of 0 leaves the KL term alone, however large r.  Where the clip holds, the first term's derivative is
+ * 0 (at r = the bound itself it does not hold).
  * A loss beyond 32 bits is infinite (a KL term with a token of probability 0, say, or a negative advantage with an r that is), and its
  * row's gradient 0.
  * moe_policy_loss_backward: the gradient alone, from the stats and the upstream gradient of every loss, grad_loss [T] fp32 (a row where
@@ -431,7 +433,7 @@ int moe_policy_loss_backward(const void* logits, int64_t ld, const int64_t* toke
  *     for rows without a token or outside all answers, whose logits are not read
  *   grad [T,V] dt (out, may be NULL): weights[i] times the gradient of loss[i] by the logits of its answers' rows; memory as in
  *     moe_distill_topk.  0 for their rows without a token; rows outside all answers (all rows, without pairs) are left as they were
- *   weights [pairs] fp32, may be NULL (1)
+ *   weights [pairs] fp32, may be NULL (1): of the gradient alone, 0 too (a row of weight 0 in moe_policy_loss has no loss either)
  * Sums over an answer are fp64, of log probabilities that are off by about 1e-7 each.  The logits are read twice where the
  * gradient is wanted: a pair's derivative needs both whole answers.
  * A token of probability 0 makes its pair's loss what the formula gives: infinite, 0, or (both answers) NaN, and the derivative with it.

@@ -794,7 +794,9 @@ def moe_policy_loss(logits, tokens, old_logprob, advantages, ref_logprob=None, c
                     temperature: float = 1.0, weights=None, gradient: bool = False, out=None):
     """loss [T], logprob [T] and stats [T,3] (fp32) of sampled tokens [T] int64 (negative: left out) under logits [T,V], from the log
     probabilities with which they were sampled, their advantages and, with `kl`, a reference's log probabilities (all [T] fp32); with
-    `gradient` also the gradient of (weights * loss).sum() by the logits, in the same pass, into `out` if given (which may be `logits`)."""
+    `gradient` also the gradient of (weights * loss).sum() by the logits, in the same pass, into `out` if given (which may be `logits`).  A row of
+    weight 0 is left out as one without a token is: its loss and log probability are 0 too.  Of logits that are views into longer rows the
+    gradient is written fastest into an `out` of the same layout, as in moe_distill_topk."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
     dev = logits.device
@@ -838,8 +840,8 @@ def moe_preference_loss(logits, tokens, offsets, ref_logprob, beta: float = 0.1,
                         gradient: bool = False, out=None):
     """loss [P], rewards [2,P], logprob [T] and stats [T,3] (fp32) of P pairs of answers: answer a is rows offsets[a] .. offsets[a+1] - 1 of
     logits [T,V], offsets [2 P + 1] int64; pair i is answers i (chosen) and P + i (rejected); tokens [T] int64 (negative: none), ref_logprob
-    [T] fp32.  With `gradient` also the gradient of (weights * loss).sum(), weights [P], by the logits, into `out` if given (which may be
-    `logits`): its rows outside all answers stay as they were in `out`, and are 0 without it."""
+    [T] fp32.  With `gradient` also the gradient of (weights * loss).sum(), weights [P] (one of 0 leaves its pair's loss), by the logits, into
+    `out` if given (which may be `logits`): its rows outside all answers stay as they were in `out`, and are 0 without it."""
     T, V, ld = _logit_rows(logits)
     dt = _dtype_code(logits)
     dev = logits.device

@@ -9,8 +9,8 @@
 //                loss = -(1 - ls) log sigmoid(h) - ls log sigmoid(-h), c = +-(ls - sigmoid(-h)) beta (over the number of tokens)
 // Bound by the read of the logits and the write of the gradient.  The policy loss knows c as soon as its row is summed, so the row stays in
 // registers and is read once; a pair's c needs all rows of both answers, so the gradient reads the logits again, last rows first.
-// us and bytes read and written: policy loss and gradient of 4096 rows of 32000 bf16 93 (5.6 TB/s); loss, then gradient of 1001 of 50001 22 (4.7) and 31
-// (6.5); pairs of 3333 rows of 32000 32 to 36 (6.2 where the call before left something in the caches), 4.9 for the 8 pairs, 63 to 67 (6.5).
+// us and bytes read and written: policy loss and gradient of 4096 rows of 32000 bf16 93 (5.6 TB/s); loss, then gradient of 1001 of 50001 22 (4.6) and 31
+// (6.5); pairs of 3333 rows of 32000 33 to 35 (6.3 where the call before left something in the caches), 4.9 for the 8 pairs, 63 (6.6).
 #include "logits_rows.h"
 
 namespace moep {
@@ -38,7 +38,7 @@ struct AnswerArgs {
   bool all_rows;                             // GRADIENT, preference: rows of no answer get 0, and are not left as they were
 };
 
-// exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, 1e-9 of the sum.)
+// exp(x) - 1 - x without the cancellation: 0.5 x^2 and up.  (Series below 0.5: the first term left out is x^10 / 10!, at most 2.2e-9 of the sum.)
 __device__ __forceinline__ float exp_beyond_line(float x) {
   if (fabsf(x) < 0.5f) {
     float s = 1.f / 362880.f;
@@ -112,8 +112,9 @@ __device__ __forceinline__ int answer_of(const int64_t* offsets, int n, int64_t 
 // Four chunks at a time, the next four on their way meanwhile, each four with a running maximum of its own: a wavefront adds up what has
 // come while the rest comes, and 32 registers of chunks leave room for twice as many wavefronts as a row that is held.  An element costs
 // the lanes seven operations (unpacked, one FMA, the exponential's four, one sum): the exponent is z c - k with k the integer next to m c, whose
-// factor exp2(k - m c) is left to the four's sum.  (c = log2(e) / tau is a number of 32 bits: sums are too large by 1.3e-8 for each unit that the
-// logits lie below the maximum.  A second FMA with what c leaves out took 3 to 7 % of the loss's time for 2e-8 of a log probability.)
+// factor exp2(k - m c) is left to the four's sum.  (c = log2(e) / tau is a number of 32 bits.  At temperature 1 it is 1.3e-8 of itself too small, and sums are
+// too large by 1.3e-8 for each unit that the logits lie below the maximum; at others the division's rounding comes in: up to 7.3e-8 for each unit of
+// (m - z) / tau, in either direction.  A second FMA with what c leaves out took 3 to 7 % of the loss's time for 2e-8 of a log probability at temperature 1.)
 constexpr int GROUP = 4;
 struct Running {
   float m = NEG_INF, s = 0.f;                // maximum, and sum of exp2((z - m) c)
@@ -406,8 +407,9 @@ __global__ __launch_bounds__(PAIR_THREADS) void pairs_kernel(PairArgs p) {
 }
 
 // Threads per row where it is not held.  us, 64 / 256 / 512 threads.  The loss alone: 1 row of 32000 bf16 - / 7.9 / 7.5; 128 of 131072 - / 18.3 / 14.6; 300 of
-// 50001 - / 14.9 / 15.5; 700 of 32000 - / 14.0 / 16.0; 1001 of 50001 - / 24.1 / 26.3.  The gradient alone: 5000 of 4000 16.5 / 18.3 / 22.5; 3256 of 32000 - / 75.5 /
-// 72.1; 8192 of 32000 - / 198 / 195.
+// 50001 - / 14.9 / 15.5; 700 of 32000 - / 14.0 / 16.0; 1001 of 50001 - / 24.1 / 26.3; 4096 of 1000 8.1 / 16.8 / -; 4096 of 4000 13.1 / 16.6 / -; 8192 of 8000
+// 30.2 / 32.0 / -, of 4000 fp32 28.2 / 26.7 / -; 1024 of 8000 12.1 / 9.6 / -; 2048 of 8000 11.7 / 12.5 / -, of 1000 6.9 / 11.0 / -.  The gradient alone: 5000 of 4000
+// 16.5 / 18.3 / 22.5; 3256 of 32000 - / 75.5 / 72.1; 8192 of 32000 - / 198 / 195.
 int threads_to_walk(int64_t T, int64_t chunks, bool gradient) {
   if (chunks <= 64 * GROUP * 4 && T > 2048) return 64;
   if (gradient) return chunks <= 512 * GROUP ? 256 : 512;

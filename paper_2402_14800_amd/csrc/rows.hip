@@ -385,7 +385,9 @@ __global__ __launch_bounds__(THREADS) void combine_rows_kernel(CombineArgs p, in
 
 // dy and dw of a token by 2^shift lanes, or by all of a workgroup of W wavefronts: each goes through its chunks of dout and of the k rows of y,
 // adding up k products in 32 bits, which are then joined in a fixed order.  A workgroup to a token has all of its loads in flight at once: rows of 8 KB,
-// 32768 tokens of 2 slots 277 us by wavefronts, 251 by workgroups, 231 past the caches; of 2 KB (4096 tokens, 2 slots) 10.8 and 11.6.
+// 32768 tokens of 2 slots 277 us by wavefronts, 251 by workgroups, 231 past the caches.  Shorter rows (bf16, 2 slots) by wavefronts / by workgroups: 1024
+// tokens of 576 6.4 / 6.4, of 1024 6.6 / 6.5, of 1536 7.6 / 6.8, of 1984 8.4 / 7.6; 2048 tokens 6.8 / 6.9, 8.6 / 8.6, 9.2 / 8.9, 10.6 / 10.4; 4096 tokens 8.9 / 9.9,
+// 11.0 / 11.4, 13.6 / 14.1, 19.3 / 19.4; 16384 tokens of 576 23 / 32, of 1984 66.6 / 65.6.
 template <typename S, int KG, int W, bool STREAM>
 __global__ __launch_bounds__(THREADS) void combine_rows_backward_kernel(CombineArgs p, int shift) {
   constexpr int N = Chunk<S>::N, U = KG > 4 ? 1 : 2;
