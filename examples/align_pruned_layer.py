@@ -38,6 +38,7 @@ class Layer:
 
     def forward(self, x):
         E = self.Wgate.shape[0]
+        # (the routing alone is wanted here: the layer's output that comes with it is thrown away, a forward pass in all)
         _, used, logits, experts = moep.moe_forward_skip_topk(x, *self.weights(), self.k, self.beta, self.kept)
         there = torch.arange(self.k, device=x.device) < used[:, None]
         weights = torch.softmax(logits.gather(1, experts.long()).masked_fill(~there, -torch.inf), 1).contiguous()
